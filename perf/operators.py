@@ -205,7 +205,8 @@ def prepare(case, seed):
     at = order.cpu()
     for b, n in enumerate(pages):
         table[b, :n] = at[cu[b]:cu[b] + n]
-    s = dict(case=case, dev=dev, new=new, cu=_cu(new), table=table.to(dev), held=torch.tensor(held, dtype=torch.int32, device=dev), room=room, spare=order[-1].long())
+    first = lens if case["op"] == "append" else [0] * len(lens)
+    s = dict(case=case, dev=dev, new=new, first=first, cu=_cu(new), table=table.to(dev), held=torch.tensor(held, dtype=torch.int32, device=dev), room=room, spare=order[-1].long())
 
     def drawn(*shape):
         # a few channels are far larger than the others, as in keys of real models
@@ -269,15 +270,13 @@ def _own(s):
     if case["op"] == "attend":
         dq.dapq_paged_attend(ctx, pages, s["cu"], s["q"], s["out"], s["lse"], softcap=case["softcap"])
         return
-    first = [0] * len(s["new"])
     if case["op"] == "append":
         q = (s["q_new"], s["q_rot"]) if case["queries"] else (None, None)
         dq.dapq_paged_append(ctx, pages, s["cu"], s["k_new"], s["v_new"], s["positions"], *q)
-        first = _lengths(case)[0]
     elif case["op"] == "compact":
         dq.dapq_paged_compact(ctx, s["k_dense"], s["v_dense"], s["cu_rows"], s["lens"], s["idx"], s["new"], pages)
     if "k_back" in s:
-        dq.dapq_paged_read(ctx, pages, first, s["new"], s["cu"][:-1], s["k_back"], s["v_back"])
+        dq.dapq_paged_read(ctx, pages, s["first"], s["new"], s["cu"][:-1], s["k_back"], s["v_back"])
 
 
 def _sequence_of(s):

@@ -18,6 +18,8 @@
  *   5. dapq_evict          1-4 for one layer's cache on one stream (dapq_evict_layers: every layer;
  *                          dapq_evict_host, dapq_evict_layers_host: the same on host buffers).
  *   Also: dapq_recall (Section 3.3, Eq. 1-3), optional pooling of the scores before step 3.
+ *   6. dapq_paged_compact, dapq_paged_append, dapq_paged_attend, dapq_paged_read: the cache that decoding goes on with
+ *      (Section 4.2 leaves its storage open), in pages, in the context's type or in 4 bits.
  *
  * Conventions
  *   - One process drives one GPU.  All kernels are asynchronous on the caller's
@@ -170,7 +172,8 @@ DAPQ_API dapq_status dapq_set_wait_limit(dapq_ctx* ctx, int64_t cycles);
 typedef enum {
   DAPQ_PROF_ROPE = 0, DAPQ_PROF_SWEEP1 = 1, DAPQ_PROF_LSE_MERGE = 2, DAPQ_PROF_SWEEP2 = 3,
   DAPQ_PROF_TOPK = 4, DAPQ_PROF_COMPACT = 5, DAPQ_PROF_POOL = 6, DAPQ_PROF_RECALL = 7, DAPQ_PROF_SLOT_SUM = 8,
-  DAPQ_PROF_KINDS = 9
+  DAPQ_PROF_PAGED_APPEND = 9, DAPQ_PROF_PAGED_READ = 10, DAPQ_PROF_PAGED_ATTEND = 11,   /* (dapq_paged_compact counts as COMPACT) */
+  DAPQ_PROF_KINDS = 12
 } dapq_prof_kind;
 DAPQ_API dapq_status dapq_profile(dapq_ctx* ctx, int32_t enable);
 DAPQ_API dapq_status dapq_profile_read(dapq_ctx* ctx, void* stream, double* ms_out, int64_t* count_out);
@@ -277,6 +280,92 @@ DAPQ_API dapq_status dapq_evict_layers_host(dapq_ctx* ctx, int32_t n_layers, con
                                    const dapq_cache_view* caches_host, const int32_t* k_keep_host,
                                    int64_t k_keep_layer_stride, void* const* k_out_host,
                                    void* const* v_out_host, int32_t* const* idx_out_host, void* stream);
+
+/* ---- the paged cache ------------------------------------------------------------------------------------------------
+ * The paper decodes on the retained rows and leaves their storage open.  Here a layer's cache is a pool of pages
+ * [n_pages][H_kv][page_rows][d] for K and one for V, and a table that says which pages a sequence has: row r of sequence b
+ * is row r % page_rows of page page_table[b][r / page_rows].  Rows are held in the context's element type, or in 4 bits:
+ *
+ *   DAPQ_CACHE_FP4: per row d / 2 bytes of codes (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; channel 2c in the low half of byte
+ *   c) and d / 16 bytes of scales (e4m3), the scale of channels 16g .. 16g + 15 at byte g:
+ *     scale = e4m3(max |x| / (6 kappa)),   code = e2m1(x / (scale kappa)),   value = code * scale * kappa,
+ *   to nearest, ties to even, largest codes where a value is beyond them; kappa = k_scale or v_scale, one number for all of K or
+ *   of V, puts the scales into e4m3's range (2^-9 .. 448; 1 does for keys and values of ordinary size).  A group with an
+ *   infinity or a NaN reads back as NaN.  72 bytes a row.
+ *
+ * The four entry points share these rules.
+ *   - cache_len (device, read by the kernels) holds the rows that each sequence has BEFORE the step's new rows, so that a
+ *     captured call can be replayed as sequences grow.  A negative entry: the sequence takes no part; none of its rows
+ *     are read or written, dapq_paged_attend gives it 0 and a log-sum-exp of -inf.
+ *   - cu_new_host: host [B + 1], new rows of sequence b are cu_new[b] .. cu_new[b + 1] - 1 (cu_new[0] = 0, none allowed); NULL:
+ *     one row each.
+ *   - A row that its sequence's part of the table has no place for, or whose page number lies outside [0, n_pages), is
+ *     skipped (dapq_paged_read writes zeros for it) and flagged: dapq_poll_status returns DAPQ_ERR_INVALID_ARG.
+ *   - No page may belong to two sequences that one call writes to.  Rows beyond those written stay as they were.
+ *   - dapq_paged_attend uses the context's workspace: the caller orders its calls on one context (one stream, or events), as
+ *     for the scorers.  The other three use none.  All are capturable and launch one kernel. */
+typedef enum { DAPQ_CACHE_NATIVE = 0, DAPQ_CACHE_FP4 = 1 } dapq_cache_format;
+
+enum { DAPQ_MIN_PAGE_ROWS = 16, DAPQ_MAX_PAGE_ROWS = 1024 };
+
+typedef struct {
+  void* k;                        /* device, [n_pages][H_kv][page_rows] rows      */
+  void* v;
+  void* k_scales;                 /* device, DAPQ_CACHE_FP4 only (else NULL)      */
+  void* v_scales;
+  int64_t page_stride;            /* channels between pages, heads, rows of K and of V alike; the codes lie at stride / 2 */
+  int64_t head_stride;            /* bytes, the scales at stride / 16.  Multiples of 16 bytes; of 128 channels for */
+  int64_t row_stride;             /* DAPQ_CACHE_FP4.  row_stride >= d             */
+  const int32_t* page_table;      /* device [B][table_stride]                     */
+  const int32_t* cache_len;       /* device [B]                                   */
+  int32_t table_stride;           /* pages that a row of the table has room for   */
+  int32_t n_pages;
+  int32_t page_rows;              /* power of two, 16 .. 1024                     */
+  int32_t format;                 /* dapq_cache_format                            */
+  float k_scale, v_scale;         /* DAPQ_CACHE_FP4: kappa, 2^-60 .. 2^60 (ignored otherwise) */
+  int32_t batch;                  /* B                                            */
+  int32_t reserved;               /* must be 0                                    */
+} dapq_paged_cache;
+
+/* The step's new tokens, T = cu_new[B] of them, heads contiguous (d apart), element type dapq_shape.dtype. */
+typedef struct {
+  const void* k;                  /* device [T, H_kv, d]                          */
+  const void* v;
+  const void* q;                  /* device [T, H_q, d] or NULL                   */
+  void* q_rot;                    /* device [T, H_q, d], contiguous; not NULL iff q is not */
+  int64_t k_token_stride, v_token_stride, q_token_stride;   /* elements, multiples of 16 bytes */
+  const int32_t* positions;       /* device [T], or NULL: k is stored as it is (q must be NULL then) */
+} dapq_new_tokens;
+
+/* Row cache_len[b] + i of sequence b becomes (RoPE(k, positions), v) of its i-th new token, with the context's frequencies and
+ * pairing: angles in double precision, products and sums in fp32, rounded once to the cache's format.  After an eviction a
+ * token's position is not the row that it takes.  With q the queries are rotated in the same launch (those of sequences that
+ * take no part too). */
+DAPQ_API dapq_status dapq_paged_append(dapq_ctx* ctx, const dapq_paged_cache* pages, const int32_t* cu_new_host,
+                              const dapq_new_tokens* tokens, void* stream);
+
+/* dapq_compact_kv into pages: the rows idx[kvh, cu_keep[b] ..] of a dense cache's K and V become the rows cache_len[b] .. of
+ * sequence b (cache_len 0: a fresh one).  idx as for dapq_compact_kv. */
+DAPQ_API dapq_status dapq_paged_compact(dapq_ctx* ctx, const dapq_cache_view* cache, const int32_t* idx,
+                               const int32_t* k_keep_host, const dapq_paged_cache* pages, void* stream);
+
+/* Rows first[b] .. first[b] + n_rows[b] - 1 of every sequence as values: k_out, v_out device [H_kv, ..] in the context's type,
+ * d contiguous, rows d apart, heads out_head_stride elements apart; sequence b's begin at row row_at[b].  That is a dense cache as
+ * dapq_score and dapq_evict take it (leave room for N synthetic rows behind each sequence).  first_host: host [B], or
+ * NULL for 0; a negative entry skips the sequence.  cache_len is not read and may be NULL. */
+DAPQ_API dapq_status dapq_paged_read(dapq_ctx* ctx, const dapq_paged_cache* pages, const int32_t* first_host,
+                            const int32_t* n_rows_host, const int32_t* row_at_host, void* k_out, void* v_out,
+                            int64_t out_head_stride, void* stream);
+
+/* out[t, h, :] = sum_j softmax_j(cap(q[t, h] . k_j * softmax_scale)) v_j over the rows j = 0 .. cache_len[b] + i that the i-th new
+ * query of sequence b sees: all that the sequence held, and the new rows up to its own (dapq_paged_append comes first).
+ * softcap: 0, or c > 0 for cap(x) = c tanh(x / c).  q: device [T, H_q, d], already rotated, tokens q_token_stride elements apart;
+ * out: device [T, H_q, d], contiguous; lse_out: device [T, H_q] natural-log sum-exp, or NULL.  Logits, maxima, sums and outputs
+ * are held in fp32; see paged_attend.cu for what the products take.  A query that sees nothing gets 0 and -inf.  Infinities
+ * and NaN in rows that no query of its sequence sees do not matter; in a row that only later queries of the same call see they may
+ * reach the earlier ones. */
+DAPQ_API dapq_status dapq_paged_attend(dapq_ctx* ctx, const dapq_paged_cache* pages, const int32_t* cu_new_host,
+                              const void* q, int64_t q_token_stride, float softcap, void* out, float* lse_out, void* stream);
 
 /* The paper has no counterpart to this entry point; it exists for callers that may not
  * allocate device memory at the point where they need scores: engines whose own allocator owns

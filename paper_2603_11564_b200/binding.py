@@ -23,6 +23,7 @@ DAPQ_OK, DAPQ_ERR_INVALID_ARG, DAPQ_ERR_UNSUPPORTED, DAPQ_ERR_WORKSPACE, DAPQ_ER
     DAPQ_ERR_TIMEOUT = range(6)
 DAPQ_BF16, DAPQ_F32 = 0, 1
 DAPQ_POOL_NONE, DAPQ_POOL_MAX, DAPQ_POOL_AVG = 0, 1, 2
+DAPQ_CACHE_NATIVE, DAPQ_CACHE_FP4 = 0, 1
 DAPQ_FLAG_CUDA_CORE_SCORER = 1
 DAPQ_FLAG_ROPE_INTERLEAVED = 2
 DAPQ_FLAG_Q_BF16, DAPQ_FLAG_Q_LO_SWEEP1, DAPQ_FLAG_Q_LO_SWEEP2 = 4, 8, 16
@@ -31,7 +32,8 @@ _STATUS_NAMES = {0: "DAPQ_OK", 1: "DAPQ_ERR_INVALID_ARG", 2: "DAPQ_ERR_UNSUPPORT
 
 EXPORTS = ("dapq_create", "dapq_destroy", "dapq_last_error", "dapq_poll_status",
            "dapq_launch_count", "dapq_set_wait_limit", "dapq_rope_inv_freq_llama3", "dapq_profile", "dapq_profile_read", "dapq_rope_pseudo_q", "dapq_score", "dapq_topk_select",
-           "dapq_compact_kv", "dapq_evict", "dapq_evict_layers", "dapq_evict_host", "dapq_evict_layers_host", "dapq_score_static", "dapq_recall")
+           "dapq_compact_kv", "dapq_evict", "dapq_evict_layers", "dapq_evict_host", "dapq_evict_layers_host", "dapq_score_static", "dapq_recall",
+           "dapq_paged_append", "dapq_paged_compact", "dapq_paged_read", "dapq_paged_attend")
 
 
 class DapqError(RuntimeError):
@@ -54,6 +56,44 @@ class dapq_cache_view(C.Structure):
                 ("v_head_stride", C.c_int64), ("v_row_stride", C.c_int64),
                 ("cu_rows_host", C.POINTER(C.c_int32)), ("prompt_len_host", C.POINTER(C.c_int32)),
                 ("batch", C.c_int32), ("reserved", C.c_int32)]
+
+
+class dapq_paged_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("page_table", C.c_void_p), ("cache_len", C.c_void_p),
+                ("table_stride", C.c_int32), ("n_pages", C.c_int32), ("page_rows", C.c_int32), ("format", C.c_int32),
+                ("k_scale", C.c_float), ("v_scale", C.c_float), ("batch", C.c_int32), ("reserved", C.c_int32)]
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, cache_len: Optional[torch.Tensor],
+                 k_scales: Optional[torch.Tensor] = None, v_scales: Optional[torch.Tensor] = None,
+                 k_scale: float = 1.0, v_scale: float = 1.0):
+        """k, v: [n_pages, H_kv, page_rows, 128] (any strides, K's and V's alike, channels contiguous); in 4 bits uint8
+        [.., 64] with k_scales, v_scales uint8 [.., 8] whose strides are an eighth of theirs.  page_table: int32
+        [B, table_stride] (rows contiguous), cache_len: int32 [B].  To be kept by the caller from step to step, it keeps the tensors."""
+        fp4 = k_scales is not None
+        per = 2 if fp4 else 1                       # channels per element of k
+        s = k.stride()
+        assert k.dim() == 4 and k.shape == v.shape and s == v.stride() and s[3] == 1 and k.shape[3] * per == 128
+        assert (k.dtype == torch.uint8) == fp4 and v.dtype == k.dtype and (v_scales is not None) == fp4
+        for x in (k_scales, v_scales) if fp4 else ():
+            assert x.element_size() == 1 and x.shape == (*k.shape[:3], 8) and x.stride(3) == 1 and all(a * 8 == b for a, b in zip(x.stride()[:3], s[:3]))
+        assert page_table.dtype == torch.int32 and page_table.dim() == 2 and (page_table.stride(1) == 1 or page_table.shape[1] == 1)
+        rows = page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1]
+        assert rows == page_table.shape[1]
+        if cache_len is not None:
+            assert cache_len.dtype == torch.int32 and cache_len.is_contiguous() and cache_len.numel() == page_table.shape[0]
+        super().__init__(k=k.data_ptr(), v=v.data_ptr(), k_scales=_ptr(k_scales), v_scales=_ptr(v_scales), page_stride=s[0] * per,
+                         head_stride=s[1] * per, row_stride=s[2] * per, page_table=page_table.data_ptr(), cache_len=_ptr(cache_len),
+                         table_stride=page_table.shape[1], n_pages=k.shape[0], page_rows=k.shape[2],
+                         format=DAPQ_CACHE_FP4 if fp4 else DAPQ_CACHE_NATIVE, k_scale=k_scale, v_scale=v_scale, batch=page_table.shape[0])
+        self.tensors = (k, v, page_table, cache_len, k_scales, v_scales)
+
+
+class dapq_new_tokens(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("q_rot", C.c_void_p),
+                ("k_token_stride", C.c_int64), ("v_token_stride", C.c_int64), ("q_token_stride", C.c_int64),
+                ("positions", C.c_void_p)]
 
 
 _lib = None
@@ -105,6 +145,15 @@ def load_library() -> C.CDLL:
     lib.dapq_evict_host.restype = C.c_int
     lib.dapq_recall.argtypes = [vp, vp, vp, i32p, i32p, C.c_int32, f32p, vp]
     lib.dapq_recall.restype = C.c_int
+    pages = C.POINTER(dapq_paged_cache)
+    lib.dapq_paged_append.argtypes = [vp, pages, i32p, C.c_void_p, vp]
+    lib.dapq_paged_append.restype = C.c_int
+    lib.dapq_paged_compact.argtypes = [vp, view, vp, i32p, pages, vp]
+    lib.dapq_paged_compact.restype = C.c_int
+    lib.dapq_paged_read.argtypes = [vp, pages, i32p, i32p, i32p, vp, vp, C.c_int64, vp]
+    lib.dapq_paged_read.restype = C.c_int
+    lib.dapq_paged_attend.argtypes = [vp, pages, i32p, vp, C.c_int64, C.c_float, vp, f32p, vp]
+    lib.dapq_paged_attend.restype = C.c_int
     lib.dapq_score_static.argtypes = [C.POINTER(dapq_shape), C.c_int, vp, view, f32p, vp,
                                       C.c_char_p, C.c_size_t]
     lib.dapq_score_static.restype = C.c_int
@@ -200,7 +249,8 @@ def dapq_launch_count(ctx) -> int:
     return int(load_library().dapq_launch_count(ctx))
 
 
-PROF_KINDS = ("rope", "sweep1", "lse_merge", "sweep2", "topk", "compact", "pool", "recall", "slot_sum")
+PROF_KINDS = ("rope", "sweep1", "lse_merge", "sweep2", "topk", "compact", "pool", "recall", "slot_sum",
+              "paged_append", "paged_read", "paged_attend")
 
 
 def dapq_rope_inv_freq_llama3(rope_base: float = 5.0e5, factor: float = 8.0, low_freq_factor: float = 1.0,
@@ -309,6 +359,53 @@ def dapq_evict_host(ctx, q_pre: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     kk, kk_p = _i32(k_keep)
     _check(ctx, load_library().dapq_evict_host(ctx, q_pre.data_ptr(), view, kk_p, k_out.data_ptr(),
                                                v_out.data_ptr(), _ptr(idx_out), _stream(stream)))
+
+
+_TOKENS = struct.Struct("@PPPPqqqP")                # dapq_new_tokens, field by field
+assert _TOKENS.size == C.sizeof(dapq_new_tokens)
+
+
+def _token_stride(x: torch.Tensor) -> int:
+    """Elements between the tokens of [T, H, 128]: heads and channels contiguous."""
+    assert x.dim() == 3 and x.shape[2] == 128 and x.stride(2) == 1 and (x.stride(1) == 128 or x.shape[1] == 1)
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * 128
+
+
+def dapq_paged_append(ctx, pages: dapq_paged_cache, cu_new, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                      q: Optional[torch.Tensor] = None, q_rot: Optional[torch.Tensor] = None, stream=None) -> None:
+    """cu_new: [B + 1] offsets of the sequences' new tokens, None: one each.  k, v: [T, H_kv, 128], q: [T, H_q, 128], e.g. slices of a
+    fused projection; q_rot: contiguous."""
+    cu, cu_p = _i32(cu_new) if cu_new is not None else (None, None)
+    assert q_rot is None or q_rot.is_contiguous()
+    tokens = _TOKENS.pack(k.data_ptr(), v.data_ptr(), _ptr(q) or 0, _ptr(q_rot) or 0, _token_stride(k), _token_stride(v),
+                          _token_stride(q) if q is not None else 0, _ptr(positions) or 0)
+    _check(ctx, load_library().dapq_paged_append(ctx, pages, cu_p, tokens, _stream(stream)))
+
+
+def dapq_paged_compact(ctx, k: torch.Tensor, v: torch.Tensor, cu_rows, prompt_len, idx: torch.Tensor, k_keep, pages: dapq_paged_cache,
+                       stream=None) -> None:
+    view, keep_alive = _view(k, v, cu_rows, prompt_len)
+    kk, kk_p = _i32(k_keep)
+    _check(ctx, load_library().dapq_paged_compact(ctx, view, idx.data_ptr(), kk_p, pages, _stream(stream)))
+
+
+def dapq_paged_read(ctx, pages: dapq_paged_cache, first, n_rows, row_at, k_out: torch.Tensor, v_out: torch.Tensor, stream=None) -> None:
+    """k_out, v_out: [H_kv, R, 128], rows contiguous, heads apart alike."""
+    hs = k_out.stride(0) if k_out.shape[0] > 1 else k_out.shape[1] * 128
+    assert k_out.dim() == 3 and k_out.shape == v_out.shape and k_out.stride() == v_out.stride() and k_out.stride()[1:] == (128, 1)
+    fi, fi_p = _i32(first) if first is not None else (None, None)
+    n, n_p = _i32(n_rows)
+    at, at_p = _i32(row_at)
+    _check(ctx, load_library().dapq_paged_read(ctx, pages, fi_p, n_p, at_p, k_out.data_ptr(), v_out.data_ptr(), hs, _stream(stream)))
+
+
+def dapq_paged_attend(ctx, pages: dapq_paged_cache, cu_new, q_rot: torch.Tensor, out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
+                      softcap: float = 0.0, stream=None) -> None:
+    """q_rot, out: [T, H_q, 128]; lse_out: [T, H_q] fp32."""
+    cu, cu_p = _i32(cu_new) if cu_new is not None else (None, None)
+    assert out.is_contiguous() and (lse_out is None or lse_out.is_contiguous())
+    _check(ctx, load_library().dapq_paged_attend(ctx, pages, cu_p, q_rot.data_ptr(), _token_stride(q_rot), softcap, out.data_ptr(), _ptr(lse_out),
+                                                 _stream(stream)))
 
 
 DAPQ_STATIC_SCRATCH_BYTES = 2 * 1024 * 1024

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "dapq_internal.cuh"
+#include "paged.cuh"
 
 using namespace dapq;
 
@@ -40,6 +41,8 @@ struct dapq_ctx {
   uint32_t* sync[2] = {};        // tickets and counters of its launches, used in turn
   int64_t sync_words = 0;
   int sync_turn = 0;
+  float* attend_part = nullptr;  // partial outputs of paged_attend.cu
+  uint32_t* attend_sync = nullptr;   // its arrival counters, all 0 between calls
   PruneBuffers prune = {};       // the pruned selection (sums == nullptr: not available)
   // staging for the host-buffer entry points (allocated on first use): two sets, so that the copies of one
   // layer run beside the kernels of the layer before
@@ -425,6 +428,8 @@ dapq_status dapq_create(dapq_ctx** out, const dapq_shape* sh, int device) {
     if (n_slots > 1) ar.add(&ctx->slots, nl * n_slots * score_bytes);
     if (flow)
       for (auto& w : ctx->sync) ar.add(&w, ctx->sync_words * sizeof(uint32_t));
+    ar.add(&ctx->attend_part, attend_part_floats(ctx->n_sm) * sizeof(float));
+    ar.add(&ctx->attend_sync, attend_sync_words(ctx->n_sm) * sizeof(uint32_t));
     return ar.allocate(ctx);
   };
   bool ok = allocate();
@@ -438,6 +443,7 @@ dapq_status dapq_create(dapq_ctx** out, const dapq_shape* sh, int device) {
   if (ok) ctx->idx = reinterpret_cast<int32_t*>(ctx->scores + (size_t)(ctx->score_slots - 1) * sh->n_kv_heads * rows);
   ok = ok && cudaMemcpy(ctx->inv_freq, freq, sizeof(freq), cudaMemcpyHostToDevice) == cudaSuccess;
   ok = ok && cudaMemset(ctx->status, 0, sizeof(int)) == cudaSuccess;
+  ok = ok && cudaMemset(ctx->attend_sync, 0, attend_sync_words(ctx->n_sm) * sizeof(uint32_t)) == cudaSuccess;
   if (!ok) { cudaGetLastError(); return bail(DAPQ_ERR_CUDA, "workspace allocation failed"); }
   if (wants_umma(ctx) && !wants_lo(ctx) && !(sh->flags & DAPQ_FLAG_Q_BF16) && sh->pool_mode == DAPQ_POOL_NONE &&
       qg_groups(ctx->dims) <= kPruneSums && (double)hq_n * rows >= kPruneLeastPairs &&
@@ -523,7 +529,9 @@ dapq_status dapq_poll_status(dapq_ctx* ctx, void* stream) {
   DAPQ_CUDA(ctx, cudaMemcpy(&word, ctx->status, sizeof(int), cudaMemcpyDeviceToHost));
   if (word) DAPQ_CUDA(ctx, cudaMemset(ctx->status, 0, sizeof(int)));
   if (word & kStatusTimeout) return fail(ctx, DAPQ_ERR_TIMEOUT, "a kernel gave up on a bounded wait; its results are undefined");
-  if (word & kStatusBadIndex) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_compact_kv skipped indices outside [0, L_b)");
+  if (word & kStatusBadPage)
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "rows of a paged cache were skipped: past the end of their page table row, or on a page outside [0, n_pages)");
+  if (word & kStatusBadIndex) return fail(ctx, DAPQ_ERR_INVALID_ARG, "a compaction (dapq_compact_kv, dapq_paged_compact) skipped indices outside [0, L_b)");
   if (word & kStatusSmemAlign)
     return fail(ctx, DAPQ_ERR_UNSUPPORTED, "the score kernels found their shared memory off a 1024-byte boundary and did nothing");
   return DAPQ_OK;
@@ -1060,6 +1068,154 @@ dapq_status dapq_evict_host(dapq_ctx* ctx, const void* q_pre_host, const dapq_ca
   if (!q_pre_host || !cache_host || !k_keep_host || !k_out_host || !v_out_host)
     return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_evict_host: NULL argument");
   return dapq_evict_layers_host(ctx, 1, &q_pre_host, cache_host, k_keep_host, 0, &k_out_host, &v_out_host, &idx_out_host, stream);
+}
+
+// ---- the paged cache --------------------------------------------------------------------------------------------------
+namespace {
+
+constexpr int64_t kMaxPagedRows = 0x7ff00000LL;    // of a sequence: row numbers stay in 32 bits
+
+dapq_status check_paged(dapq_ctx* ctx, const char* who, const dapq_paged_cache* pc, bool need_len, PagedDev* out) {
+  if (!pc) return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: the paged cache is NULL", who);
+  if (pc->format != DAPQ_CACHE_NATIVE && pc->format != DAPQ_CACHE_FP4) return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: unknown cache format %d", who, pc->format);
+  const bool fp4 = pc->format == DAPQ_CACHE_FP4;
+  if (!pc->k || !pc->v || !pc->page_table || (need_len && !pc->cache_len) || (fp4 && (!pc->k_scales || !pc->v_scales)))
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: the paged cache has a NULL pointer", who);
+  if (pc->reserved != 0) return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: reserved field of the paged cache must be 0", who);
+  if (pc->batch < 1) return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: batch must be >= 1 (got %d)", who, pc->batch);
+  if (pc->batch > ctx->shape.max_batch) return fail(ctx, DAPQ_ERR_WORKSPACE, "%s: batch %d exceeds max_batch %d", who, pc->batch, ctx->shape.max_batch);
+  if (pc->n_pages < 1 || pc->table_stride < 1) return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: n_pages and table_stride must be >= 1", who);
+  if (pc->page_rows < DAPQ_MIN_PAGE_ROWS || pc->page_rows > DAPQ_MAX_PAGE_ROWS || (pc->page_rows & (pc->page_rows - 1)))
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: page_rows must be a power of two in 16 .. 1024 (got %d)", who, pc->page_rows);
+  if ((int64_t)pc->table_stride * pc->page_rows > kMaxPagedRows)
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: a sequence's table has room for more than %lld rows", who, (long long)kMaxPagedRows);
+  if (pc->row_stride < kHeadDim || pc->head_stride < 0 || pc->page_stride < 0)
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: row_stride must be >= head_dim, head_stride and page_stride >= 0", who);
+  const int64_t unit = fp4 ? kHeadDim : 16 / ctx->elem_bytes;
+  const bool scales_ok = !fp4 || (((uintptr_t)pc->k_scales | (uintptr_t)pc->v_scales) & 7u) == 0;
+  if (pc->page_stride % unit || pc->head_stride % unit || pc->row_stride % unit || !aligned16(pc->k) || !aligned16(pc->v) || !scales_ok)
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: pages must lie on 16-byte boundaries (scales: 8) with strides of whole %s", who,
+                fp4 ? "multiples of 128 channels" : "16 bytes");
+  if (fp4 && !(pc->k_scale >= 0x1p-60f && pc->k_scale <= 0x1p60f && pc->v_scale >= 0x1p-60f && pc->v_scale <= 0x1p60f))
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: k_scale and v_scale must be in 2^-60 .. 2^60", who);
+  int shift = 0;
+  while ((1 << shift) < pc->page_rows) ++shift;
+  *out = {(char*)pc->k, (char*)pc->v, (unsigned char*)pc->k_scales, (unsigned char*)pc->v_scales, pc->page_stride, pc->head_stride, pc->row_stride,
+          pc->page_table, pc->cache_len, pc->table_stride, pc->n_pages, shift, fp4 ? 1 : 0, pc->k_scale, pc->v_scale};
+  return DAPQ_OK;
+}
+
+dapq_status check_new_rows(dapq_ctx* ctx, const char* who, int32_t batch, const int32_t* cu, NewRows* t) {
+  memset(t, 0, sizeof(*t));
+  t->batch = batch;
+  for (int b = 0; b <= batch; ++b) {
+    t->cu[b] = cu ? cu[b] : b;
+    if (b == 0 ? t->cu[0] != 0 : t->cu[b] < t->cu[b - 1])
+      return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: cu_new must begin with 0 and not fall (cu_new[%d] = %d)", who, b, t->cu[b]);
+  }
+  if ((int64_t)t->cu[batch] * ctx->dims.n_q_heads > 0x7fffffffLL)
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: %d new tokens with %d heads are too many for one call", who, t->cu[batch], ctx->dims.n_q_heads);
+  return DAPQ_OK;
+}
+
+}  // namespace
+
+dapq_status dapq_paged_append(dapq_ctx* ctx, const dapq_paged_cache* pages, const int32_t* cu_new_host, const dapq_new_tokens* nt, void* stream) {
+  if (!ctx) return DAPQ_ERR_INVALID_ARG;
+  PagedDev pg;
+  NewRows t;
+  dapq_status st = check_paged(ctx, "dapq_paged_append", pages, true, &pg);
+  if (st == DAPQ_OK) st = check_new_rows(ctx, "dapq_paged_append", pages->batch, cu_new_host, &t);
+  if (st != DAPQ_OK) return st;
+  if (!nt || !nt->k || !nt->v || (nt->q != nullptr) != (nt->q_rot != nullptr))
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_append: new tokens need k and v, and q_rot if and only if they have q");
+  if (nt->q && !nt->positions) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_append: q needs positions");
+  const int per16 = 16 / ctx->elem_bytes;
+  const int64_t kv = (int64_t)ctx->dims.n_kv_heads * kHeadDim, q = (int64_t)ctx->dims.n_q_heads * kHeadDim;
+  if (nt->k_token_stride < kv || nt->v_token_stride < kv || (nt->q && nt->q_token_stride < q))
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_append: token strides must be at least a token's heads");
+  if (!aligned16(nt->k) || !aligned16(nt->v) || nt->k_token_stride % per16 || nt->v_token_stride % per16 ||
+      (nt->q && (!aligned16(nt->q) || !aligned16(nt->q_rot) || nt->q_token_stride % per16)))
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "dapq_paged_append: new tokens must lie on 16-byte boundaries, with strides of whole 16 bytes");
+  if (t.cu[t.batch] == 0) return DAPQ_OK;
+  DeviceGuard guard(ctx->device);
+  const NewTokensDev dev = {nt->k, nt->v, nt->q, nt->q_rot, nt->k_token_stride, nt->v_token_stride, nt->q_token_stride, nt->positions};
+  cudaError_t e = launch_paged_append(ctx->shape.dtype, pg, t, dev, ctx->inv_freq, ctx->dims, ctx->status, (cudaStream_t)stream, &ctx->log);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "paged append kernel");
+  return DAPQ_OK;
+}
+
+dapq_status dapq_paged_compact(dapq_ctx* ctx, const dapq_cache_view* cache, const int32_t* idx, const int32_t* k_keep_host,
+                               const dapq_paged_cache* pages, void* stream) {
+  if (!ctx) return DAPQ_ERR_INVALID_ARG;
+  if (!idx || !k_keep_host) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_compact: NULL argument");
+  PagedDev pg;
+  CacheDev cd;
+  SeqTable t;
+  dapq_status st = check_paged(ctx, "dapq_paged_compact", pages, true, &pg);
+  if (st == DAPQ_OK) st = check_view(ctx, cache, true, false, &cd);
+  if (st == DAPQ_OK && cache->batch != pages->batch)
+    st = fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_compact: %d sequences in the dense cache, %d in the paged one", cache->batch, pages->batch);
+  if (st == DAPQ_OK) st = build_table(ctx, cache->batch, cache->cu_rows_host, cache->prompt_len_host, nullptr, k_keep_host, nullptr, &t);
+  if (st != DAPQ_OK) return st;
+  DeviceGuard guard(ctx->device);
+  cudaError_t e = launch_paged_compact(ctx->shape.dtype, pg, cd, idx, t, ctx->dims.n_kv_heads, ctx->status, (cudaStream_t)stream, &ctx->log);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "paged compaction kernel");
+  return DAPQ_OK;
+}
+
+dapq_status dapq_paged_read(dapq_ctx* ctx, const dapq_paged_cache* pages, const int32_t* first_host, const int32_t* n_rows_host,
+                            const int32_t* row_at_host, void* k_out, void* v_out, int64_t out_head_stride, void* stream) {
+  if (!ctx) return DAPQ_ERR_INVALID_ARG;
+  if (!n_rows_host || !row_at_host || !k_out || !v_out) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_read: NULL argument");
+  PagedDev pg;
+  const dapq_status st = check_paged(ctx, "dapq_paged_read", pages, false, &pg);
+  if (st != DAPQ_OK) return st;
+  ReadRows t;
+  memset(&t, 0, sizeof(t));
+  t.rows.batch = pages->batch;
+  int64_t total = 0;
+  for (int b = 0; b < pages->batch; ++b) {
+    const int64_t n = first_host && first_host[b] < 0 ? 0 : n_rows_host[b];
+    if (n_rows_host[b] < 0 || row_at_host[b] < 0) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_read: n_rows[%d] or row_at[%d] is negative", b, b);
+    if (((int64_t)row_at_host[b] + n) * kHeadDim > out_head_stride)
+      return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_read: rows of sequence %d end behind out_head_stride", b);
+    t.first[b] = first_host ? first_host[b] : 0;
+    t.row_at[b] = row_at_host[b];
+    t.rows.cu[b] = (int32_t)total;
+    total += n;
+    if (total > 0x7fffffffLL) return fail(ctx, DAPQ_ERR_UNSUPPORTED, "dapq_paged_read: more than 2^31 - 1 rows");
+  }
+  t.rows.cu[pages->batch] = (int32_t)total;
+  if (!aligned16(k_out) || !aligned16(v_out) || out_head_stride % (16 / ctx->elem_bytes))
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "dapq_paged_read: k_out and v_out must lie on 16-byte boundaries, heads whole 16 bytes apart");
+  if (total == 0) return DAPQ_OK;
+  DeviceGuard guard(ctx->device);
+  cudaError_t e = launch_paged_read(ctx->shape.dtype, pg, t, ctx->dims.n_kv_heads, k_out, v_out, out_head_stride, ctx->status, (cudaStream_t)stream, &ctx->log);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "paged read kernel");
+  return DAPQ_OK;
+}
+
+dapq_status dapq_paged_attend(dapq_ctx* ctx, const dapq_paged_cache* pages, const int32_t* cu_new_host, const void* q, int64_t q_token_stride,
+                              float softcap, void* out, float* lse_out, void* stream) {
+  if (!ctx) return DAPQ_ERR_INVALID_ARG;
+  if (!q || !out) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_attend: NULL argument");
+  PagedDev pg;
+  NewRows t;
+  dapq_status st = check_paged(ctx, "dapq_paged_attend", pages, true, &pg);
+  if (st == DAPQ_OK) st = check_new_rows(ctx, "dapq_paged_attend", pages->batch, cu_new_host, &t);
+  if (st != DAPQ_OK) return st;
+  if (!(softcap >= 0.f && softcap <= 3.0e38f)) return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_attend: softcap must be 0 or a finite positive number");
+  if (q_token_stride < (int64_t)ctx->dims.n_q_heads * kHeadDim)
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_attend: q_token_stride must be at least a token's heads");
+  if (!aligned16(q) || !aligned16(out) || q_token_stride % (16 / ctx->elem_bytes))
+    return fail(ctx, DAPQ_ERR_UNSUPPORTED, "dapq_paged_attend: q and out must lie on 16-byte boundaries, tokens whole 16 bytes apart");
+  if (t.cu[t.batch] == 0) return DAPQ_OK;
+  DeviceGuard guard(ctx->device);
+  cudaError_t e = launch_paged_attend(ctx->shape.dtype, pg, t, ctx->dims, q, q_token_stride, softcap, out, lse_out, ctx->attend_part, ctx->attend_sync, ctx->n_sm,
+                                      ctx->status, (cudaStream_t)stream, &ctx->log);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "paged attention kernel");
+  return DAPQ_OK;
 }
 
 }  // extern "C"

@@ -50,7 +50,7 @@ struct Dims {
 };
 
 // Device status word bits (set by kernels, read by dapq_poll_status).
-enum : int { kStatusTimeout = 1, kStatusBadIndex = 2, kStatusSmemAlign = 4 };
+enum : int { kStatusTimeout = 1, kStatusBadIndex = 2, kStatusSmemAlign = 4, kStatusBadPage = 8 };
 
 // Output formats of the rotation kernel.
 enum : int { kRopeOutBf16 = DAPQ_BF16, kRopeOutF32 = DAPQ_F32, kRopeOutSplitBf16 = 2, kRopeOutF16 = 3 };
@@ -67,7 +67,7 @@ __device__ __forceinline__ int find_segment(const int32_t* cu, int n, int x) {
 
 // Kernel kinds, for launch accounting and the optional per-kernel event timing.
 enum KernelKind : int { kKindRope = 0, kKindSweep1, kKindLseMerge, kKindSweep2, kKindTopk, kKindCompact, kKindPool,
-                        kKindRecall, kKindSlotSum, kKindCount };
+                        kKindRecall, kKindSlotSum, kKindPagedAppend, kKindPagedRead, kKindPagedAttend, kKindCount };
 
 // Counts launches and, while profiling is on, brackets every launch with CUDA events on
 // the launching stream (implemented in api.cu; events come from a host-side pool).

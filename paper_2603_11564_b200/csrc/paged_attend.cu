@@ -1,0 +1,797 @@
+// Attention over the paged cache: out = softmax(cap(q K^T scale)) V for the step's new queries, which see what their sequence held and the new rows up to
+// their own.
+//
+// One token of a sequence reads the whole cache of its KV heads for G query rows: 4 G flops a byte in bf16, 14 G in 4 bits.  What
+// bounds it is the stream of cache rows, and in 4 bits also the instructions that turn codes into operands, 256 values a row
+// and head at 40 values a cycle and SM; so operands go from shared memory through registers straight into warp-level MMAs, with the
+// KEYS (then the channels of V) as the tall side and the query rows as the narrow one (n = 8), which wastes nothing on a group of
+// 8 or fewer.  Tensor memory would need the operands written once more than they are read.
+//
+// Work: (sequence, KV head, query row tile, tile of kWarps * 16 keys), numbered in this order.  Lengths are known on the device
+// only, so every CTA of one wave adds them up and takes an equal run of the numbers, whatever the lengths are.  Of its run's tiles a warp
+// takes 16 keys each, with its own copies in flight, its own running maxima and sums; a CTA's warps are joined when its run
+// leaves a unit (sequence, head, row tile), and the CTAs of a unit that several share by the one of them that is last to arrive, in CTA order, so that
+// the result does not depend on who that is.  Nobody waits for another CTA.
+//
+// Softmax: base 2, against a maximum that is only moved when a logit exceeds it by more than kSlack, so that most tiles need neither
+// a reduction nor a rescaling.
+#include "paged.cuh"
+#include "umma_ptx.cuh"
+
+namespace dapq {
+namespace {
+
+using ptx::ex2;
+using ptx::smem_u32;
+
+constexpr int kWarpKeys = 16;
+constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
+constexpr int kPadRow = 132;                         // floats of a row of the warps' partial outputs (conflict-free, see flush)
+constexpr int kMaxRows = 16, kPartRow = kHeadDim + 2, kMaxCtasPerSm = 2;
+
+struct Attend {
+  PagedDev pg;
+  NewRows t;
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  float *lse, *part;
+  uint32_t* sync;
+  int* status;
+  int32_t n_q_heads, n_kv_heads, group;
+  float scale_log2e, softcap;
+};
+
+// ---- pieces ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float4 lds_f4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
+__device__ __forceinline__ __half2 halves(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+template <bool kF16>
+__device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (kF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// c tanh(x / c) log2(e) of x = y c / (2 log2(e)), through the exponential (the tanh instruction has 11 bits).
+__device__ __forceinline__ float capped(float y, float c_log2e) { return c_log2e - __fdividef(2.f * c_log2e, 1.f + ex2(y)); }
+
+// What a unit is: a row tile of one sequence and KV head.
+struct Unit {
+  int b, h, row0;          // first query row; row r is query r / group of the sequence, head h * group + r % group
+  int rows;                // rows of the sequence
+  int held, limit;         // rows held before the step, end of the rows that any of the tile's queries sees
+  int full;                // end of the rows that all of them see
+  int64_t table;           // its row of the page table
+};
+
+// Walks the CTA's run of tiles.
+struct Cursor {
+  int64_t pos, end;
+  int b, unit, tile, tiles, units;
+};
+
+// The geometry that every CTA works out for itself, in shared memory.
+struct Shape {
+  int64_t before[kMaxBatch + 1];                     // tiles of the sequences before
+};
+
+template <class E>
+__device__ __forceinline__ int tiles_of(const Attend& a, int b, int* units) {
+  const int n = a.t.cu[b + 1] - a.t.cu[b], held = a.pg.len[b];
+  *units = a.n_kv_heads * ((n * a.group + E::kRows - 1) / E::kRows);
+  const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift, rows = held < 0 ? 0 : min((int64_t)held + n, room);
+  return n == 0 ? 0 : max(1, (int)((rows + E::kTile - 1) / E::kTile));
+}
+
+template <class E>
+__device__ __forceinline__ void enter(const Attend& a, Cursor& c) {     // c.b is set; skips sequences without tiles
+  while (c.b < a.t.batch) {
+    c.tiles = tiles_of<E>(a, c.b, &c.units);
+    if (c.tiles > 0) break;
+    ++c.b;
+  }
+}
+template <class E>
+__device__ __forceinline__ void advance(const Attend& a, Cursor& c) {
+  ++c.pos;
+  if (++c.tile == c.tiles) {
+    c.tile = 0;
+    if (++c.unit == c.units && c.pos < c.end) {
+      c.unit = 0;
+      ++c.b;
+      enter<E>(a, c);
+    }
+  }
+}
+template <class E>
+__device__ __forceinline__ Unit unit_of(const Attend& a, const Cursor& c) {
+  Unit u;
+  u.b = c.b;
+  const int n = a.t.cu[c.b + 1] - a.t.cu[c.b];
+  u.rows = n * a.group;
+  const int tiles = (u.rows + E::kRows - 1) / E::kRows;
+  u.h = c.unit / tiles;
+  u.row0 = (c.unit - u.h * tiles) * E::kRows;
+  u.held = a.pg.len[c.b];
+  const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift;
+  const int first = u.row0 / a.group, last = min((u.row0 + E::kRows - 1) / a.group, n - 1);
+  u.limit = u.held < 0 ? 0 : (int)min((int64_t)u.held + last + 1, room);
+  u.full = u.held < 0 ? 0 : (int)min((int64_t)u.held + first + 1, room);
+  u.table = (int64_t)c.b * a.pg.table_stride;
+  return u;
+}
+// Rows that query row r of the unit sees.
+__device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
+  const int row = u.row0 + r;
+  return row < u.rows && u.held >= 0 ? (int)min((int64_t)u.held + row / a.group + 1, (int64_t)u.limit) : 0;
+}
+
+// ---- 16 keys of a warp on the tensor cores ----------------------------------------------------------------------------
+// Products: S^T = K Q^T, m16n8k16 with the 16 keys as rows; O^T += V^T P^T with 16 channels as rows and the keys as k.  Which key is row r of the
+// one and index r of the other is free as long as it is the same, and so is which channel is which index of the contraction:
+// key_of makes the shared-memory reads of both conflict-free, and each thread's channels are consecutive in memory.
+// fp16 for 4-bit caches: codes times scales are exact in it (6 significant bits), queries too once each row is scaled by a power of two, and
+// the weights, 2^11 times what they are, are rounded to 11 bits.  bf16 for bf16 caches: keys, values and queries exact, weights rounded to
+// 8 bits (2^-9 of each, of either sign; the sum of the weights is that of the unrounded ones).
+template <bool kFp4, int kTiles>
+struct TensorEngine {
+  static constexpr int kNT = kTiles;
+  static constexpr int kWarps = 8, kTile = kWarps * kWarpKeys, kRows = 8 * kNT, kCtas = kFp4 && kNT == 1 ? 2 : 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kStageBytes = kFp4 ? kWarpKeys * 144 : kWarpKeys * 512;
+  static constexpr int kExtra = 0;
+  static constexpr float kLift = kFp4 ? 11.f : 0.f;
+  using T = __nv_bfloat16;
+
+  uint32_t q[kNT][16];
+  float o[kNT][8][4], m[kNT][2], l[kNT][2], fac[kNT][2];
+  int lim[kNT][2];
+
+  __device__ __forceinline__ static int key_of(int r) { return (r & 8) + ((r & 1) ? 4 + (((r & 7) >> 1) ^ 1) : (r & 7) >> 1); }
+  // 4 bits: a row is 4 pieces of 16 bytes, bf16: 16 pieces; where piece c of row r lies
+  __device__ __forceinline__ static int piece4(int r, int c) { return r * 64 + ((c ^ (((r >> 1) & 1) << 1)) << 4); }
+  __device__ __forceinline__ static int piece16(int r, int c) { return r * 256 + ((c ^ (((r & 3) << 1) | ((r >> 2) & 1))) << 4); }
+
+  // Rows of the stage: off is the channel offset of the tile's first row.
+  __device__ __forceinline__ static void issue(const Attend& a, uint32_t stage, int64_t off, int lane) {
+    const int64_t step = a.pg.row_stride;
+    if (kFp4) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = (lane >> 2) + 8 * j, c = lane & 3;
+        const int64_t at = (off + r * step) / 2 + c * 16;
+        ptx::cp_async16(stage + piece4(r, c), a.pg.k + at);
+        ptx::cp_async16(stage + 1024 + piece4(r, c), a.pg.v + at);
+      }
+      const int r = lane & 15;
+      cp_async8(stage + 2048 + 8 * lane, (lane < 16 ? a.pg.k_scales : a.pg.v_scales) + (off + r * step) / 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int r = (lane >> 4) + 2 * j, c = lane & 15;
+        const int64_t at = (off + r * step) * 2 + c * 16;
+        ptx::cp_async16(stage + piece16(r, c), a.pg.k + at);
+        ptx::cp_async16(stage + 4096 + piece16(r, c), a.pg.v + at);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void begin(const Attend& a, const Unit& u, unsigned char*, int, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      const int r = 8 * nt + g, row = u.row0 + r;
+      uint4 w[4] = {};
+      if (row < u.rows) {
+        const int i = row / a.group, h = u.h * a.group + row - i * a.group;
+        const uint4* src = reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(a.t.cu[u.b] + i) * a.q_stride + h * kHeadDim);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = __ldg(src + (kFp4 ? 4 * t + j : 2 * t + (j & 1) + 8 * (j >> 1)));
+      }
+      const uint32_t* raw = reinterpret_cast<const uint32_t*>(w);
+      float back = 1.f;
+      if (kFp4) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = max(top, max((raw[i] << 16) & 0x7fffffffu, raw[i] & 0x7fff0000u));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = top == 0 ? 127 : min(max((int)(top >> 23), 1), 253);
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+        back = __uint_as_float((uint32_t)e << 23);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          q[nt][i] = bits(__floats2half2_rn(__uint_as_float(raw[i] << 16) * down, __uint_as_float(raw[i] & 0xffff0000u) * down));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) q[nt][i] = raw[i];
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        fac[nt][e] = a.scale_log2e * (kFp4 ? __shfl_sync(0xffffffffu, back, (2 * t + e) * 4) * a.pg.k_scale : 1.f);
+        if (a.softcap > 0.f) fac[nt][e] *= 2.f / a.softcap;
+        lim[nt][e] = sees(a, u, 8 * nt + 2 * t + e);
+        m[nt][e] = kLowest;
+        l[nt][e] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][j][e] = 0.f;
+    }
+  }
+
+  // Keys base .. base + 15 of the sequence; whole: all of the tile's queries see all of them.
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, bool whole, unsigned char*, int, int lane) {
+    const int g = lane >> 2, t = lane & 3, rk = key_of(g);
+    float s[kNT][4];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+    if (kFp4) {
+      const uint4 ka = ptx::lds128(stage + piece4(rk, t)), kb = ptx::lds128(stage + piece4(rk + 8, t));
+      const __half2 sa = scales_to_half2(lds_u16(stage + 2048 + 8 * rk + 2 * t)), sb = scales_to_half2(lds_u16(stage + 2048 + 8 * rk + 64 + 2 * t));
+      const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const __half2 fa = w < 2 ? __low2half2(sa) : __high2half2(sa), fb = w < 2 ? __low2half2(sb) : __high2half2(sb);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const uint32_t a0 = bits(__hmul2(fp4x2_to_half2((wa[w] >> (16 * p)) & 255u), fa)), a2 = bits(__hmul2(fp4x2_to_half2((wa[w] >> (16 * p + 8)) & 255u), fa));
+          const uint32_t a1 = bits(__hmul2(fp4x2_to_half2((wb[w] >> (16 * p)) & 255u), fb)), a3 = bits(__hmul2(fp4x2_to_half2((wb[w] >> (16 * p + 8)) & 255u), fb));
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) mma<true>(s[nt], a0, a1, a2, a3, q[nt][4 * w + 2 * p], q[nt][4 * w + 2 * p + 1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = 2 * t + (j & 1) + 8 * (j >> 1);
+        const uint4 ka = ptx::lds128(stage + piece16(rk, c)), kb = ptx::lds128(stage + piece16(rk + 8, c));
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+          mma<false>(s[nt], ka.x, kb.x, ka.y, kb.y, q[nt][4 * j], q[nt][4 * j + 1]);
+          mma<false>(s[nt], ka.z, kb.z, ka.w, kb.w, q[nt][4 * j + 2], q[nt][4 * j + 3]);
+        }
+      }
+    }
+    // base-2 logits
+    float z[kNT][4];
+    bool above = false;
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        z[nt][e] = s[nt][e] * fac[nt][e & 1];
+        if (a.softcap > 0.f) z[nt][e] = capped(z[nt][e], a.softcap * 1.44269504f);
+        if (!whole && base + rk + (e & 2) * 4 >= lim[nt][e & 1]) z[nt][e] = -CUDART_INF_F;
+        above = above || z[nt][e] > m[nt][e & 1] + kSlack;
+      }
+    if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(z[nt][e], z[nt][e + 2]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+          top = fmaxf(top, m[nt][e]);
+          const float f = ex2(m[nt][e] - top);
+          m[nt][e] = top;
+          l[nt][e] *= f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            o[nt][j][e] *= f;
+            o[nt][j][e + 2] *= f;
+          }
+        }
+    }
+    uint32_t p0[kNT], p1[kNT];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = ex2(z[nt][e] - m[nt][e & 1] + kLift);
+        l[nt][e & 1] += p[e];
+      }
+      uint32_t lo, hi;
+      if (kFp4) {
+        lo = bits(__floats2half2_rn(p[0], p[1]));
+        hi = bits(__floats2half2_rn(p[2], p[3]));
+      } else {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
+        lo = *reinterpret_cast<const uint32_t*>(&x);
+        hi = *reinterpret_cast<const uint32_t*>(&y);
+      }
+      p0[nt] = transpose8x8(lo);
+      p1[nt] = transpose8x8(hi);
+    }
+    // indices 2t, 2t + 1, 2t + 8, 2t + 9 of the contraction; rows behind the last visible one may hold anything
+    const int rv[4] = {t, 4 + (t ^ 1), 8 + t, 12 + (t ^ 1)};
+    if (kFp4) {
+      uint32_t w[4][2], sc[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 x = lds64(stage + 1024 + piece4(rv[i], g >> 1) + 8 * (g & 1));
+        w[i][0] = x.x;
+        w[i][1] = x.y;
+        sc[i] = lds_u8(stage + 2176 + 8 * rv[i] + g);
+        if (!whole && base + rv[i] >= u.limit) sc[i] = 0;
+      }
+      const __half2 f01 = scales_to_half2(sc[0] | (sc[1] << 8)), f23 = scales_to_half2(sc[2] | (sc[3] << 8));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = bits(fp4x2_to_half2((w[i][j >> 2] >> (8 * (j & 3))) & 255u));
+        const uint32_t a0 = bits(__hmul2(halves(__byte_perm(x[0], x[1], 0x5410)), f01)), a1 = bits(__hmul2(halves(__byte_perm(x[0], x[1], 0x7632)), f01));
+        const uint32_t a2 = bits(__hmul2(halves(__byte_perm(x[2], x[3], 0x5410)), f23)), a3 = bits(__hmul2(halves(__byte_perm(x[2], x[3], 0x7632)), f23));
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) mma<true>(o[nt][j], a0, a1, a2, a3, p0[nt], p1[nt]);
+      }
+    } else {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        uint4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[i] = ptx::lds128(stage + 4096 + piece16(rv[i], g + 8 * hf));
+          if (!whole && base + rv[i] >= u.limit) w[i] = make_uint4(0, 0, 0, 0);
+        }
+        const uint32_t* x[4] = {&w[0].x, &w[1].x, &w[2].x, &w[3].x};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t a0 = __byte_perm(x[0][j], x[1][j], 0x5410), a1 = __byte_perm(x[0][j], x[1][j], 0x7632);
+          const uint32_t a2 = __byte_perm(x[2][j], x[3][j], 0x5410), a3 = __byte_perm(x[2][j], x[3][j], 0x7632);
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) mma<false>(o[nt][4 * hf + j], a0, a1, a2, a3, p0[nt], p1[nt]);
+        }
+      }
+    }
+  }
+
+  // The warp's outputs of rows 8 nt .. 8 nt + 7 to buf [8][kPadRow] at position 16 j + 2 g + e, its maxima and sums to ml [8].
+  __device__ __forceinline__ void flush(float* buf, float2* ml, int nt, int lane) const {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+      if (n != nt) continue;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float sum = l[n][e];
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        if (g == 0) ml[2 * t + e] = make_float2(m[n][e], sum);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<float2*>(buf + (2 * t + e) * kPadRow + 16 * j + 2 * g) = make_float2(o[n][j][e], o[n][j][e + 2]);
+      }
+    }
+  }
+  // First of the two channels at positions p, p + 1 (p even).
+  __device__ __forceinline__ static int channel(int p) {
+    const int j = p >> 4, g = (p >> 1) & 7;
+    return kFp4 ? 16 * g + 2 * j : 64 * (j >> 2) + 8 * g + 2 * (j & 3);
+  }
+};
+
+// ---- 16 keys of a warp in fp32 on the CUDA cores -----------------------------------------------------------------------
+// For fp32 contexts, nothing is rounded below fp32: two lanes a key for the logits (each half of its channels), four channels a lane for the
+// outputs, queries and weights broadcast from shared memory.
+template <bool kFp4>
+struct FloatEngine {
+  static constexpr int kWarps = 4, kTile = kWarps * kWarpKeys, kRows = 8, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kStageBytes = kFp4 ? kWarpKeys * 144 : kWarpKeys * 1024;
+  static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = kWarpKeys * kRows * 4;
+  static constexpr int kExtra = kQBytes + kWarps * kPBytes;
+  static constexpr float kLift = 0.f;
+  static constexpr int kNT = 1;
+  using T = float;
+
+  float o[kRows][4], m[kRows], l[kRows / 2], fac;
+
+  __device__ __forceinline__ static int piece4(int r, int c) { return TensorEngine<true, 1>::piece4(r, c); }
+  __device__ __forceinline__ static int piece32(int r, int c) { return r * 512 + ((c ^ ((r & 3) << 1)) << 4); }
+
+  __device__ __forceinline__ static void issue(const Attend& a, uint32_t stage, int64_t off, int lane) {
+    if (kFp4) {
+      TensorEngine<true, 1>::issue(a, stage, off, lane);
+    } else {
+#pragma unroll
+      for (int r = 0; r < kWarpKeys; ++r) {
+        const int64_t at = (off + r * a.pg.row_stride) * 4 + lane * 16;
+        ptx::cp_async16(stage + piece32(r, lane), a.pg.k + at);
+        ptx::cp_async16(stage + 8192 + piece32(r, lane), a.pg.v + at);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void begin(const Attend& a, const Unit& u, unsigned char* extra, int, int) {
+    for (int x = threadIdx.x; x < kRows * kHeadDim / 4; x += kWarps * 32) {
+      const int row = u.row0 + x / (kHeadDim / 4), i = row / a.group, h = u.h * a.group + row - i * a.group;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row < u.rows) v = __ldg(reinterpret_cast<const float4*>((const T*)a.q + (int64_t)(a.t.cu[u.b] + i) * a.q_stride + h * kHeadDim) + x % (kHeadDim / 4));
+      reinterpret_cast<float4*>(extra)[x] = v;
+    }
+    __syncthreads();
+    fac = a.scale_log2e * (kFp4 ? a.pg.k_scale : 1.f) * (a.softcap > 0.f ? 2.f / a.softcap : 1.f);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      m[r] = kLowest;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[r][e] = 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < kRows / 2; ++r) l[r] = 0.f;
+  }
+
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, bool whole, unsigned char* extra, int warp, int lane) {
+    const int key = lane >> 1, hf = lane & 1;
+    const uint32_t qs = smem_u32(extra), ps = qs + kQBytes + warp * kPBytes;
+    float s[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) s[r] = 0.f;
+    if (kFp4) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {                                       // groups 4 hf + p of 16 channels
+        const uint2 w = lds64(stage + piece4(key, 2 * hf + (p >> 1)) + 8 * (p & 1));
+        const float f = scale_to_float(lds_u8(stage + 2048 + 8 * key + 4 * hf + p));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {                                     // four channels
+          const uint32_t two = (c < 2 ? w.x : w.y) >> (16 * (c & 1));
+          const float2 x = __half22float2(fp4x2_to_half2(two & 255u)), y = __half22float2(fp4x2_to_half2((two >> 8) & 255u));
+#pragma unroll
+          for (int r = 0; r < kRows; ++r) {
+            const float4 qv = lds_f4(qs + r * kHeadDim * 4 + (64 * hf + 16 * p + 4 * c) * 4);
+            s[r] = fmaf(f * x.x, qv.x, fmaf(f * x.y, qv.y, fmaf(f * y.x, qv.z, fmaf(f * y.y, qv.w, s[r]))));
+          }
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int c = 0; c < 16; ++c) {
+        const float4 kv = lds_f4(stage + piece32(key, 2 * c + hf));
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          const float4 qv = lds_f4(qs + r * kHeadDim * 4 + (2 * c + hf) * 16);
+          s[r] = fmaf(kv.x, qv.x, fmaf(kv.y, qv.y, fmaf(kv.z, qv.z, fmaf(kv.w, qv.w, s[r]))));
+        }
+      }
+    }
+    float z[kRows / 2];
+    bool above = false;
+#pragma unroll
+    for (int i = 0; i < kRows / 2; ++i) {                                 // this lane's rows: 2 i + hf
+      const float s0 = s[2 * i] + __shfl_xor_sync(0xffffffffu, s[2 * i], 1), s1 = s[2 * i + 1] + __shfl_xor_sync(0xffffffffu, s[2 * i + 1], 1);
+      z[i] = (hf ? s1 : s0) * fac;
+      if (a.softcap > 0.f) z[i] = capped(z[i], a.softcap * 1.44269504f);
+      if (!whole && base + key >= sees(a, u, 2 * i + hf)) z[i] = -CUDART_INF_F;
+      above = above || z[i] > (hf ? m[2 * i + 1] : m[2 * i]) + kSlack;
+    }
+    if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+      for (int i = 0; i < kRows / 2; ++i) {
+        float top = z[i];
+#pragma unroll
+        for (int x = 2; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        const float other = __shfl_xor_sync(0xffffffffu, top, 1);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int r = 2 * i + e;
+          const float mine = fmaxf(e == hf ? top : other, m[r]), f = ex2(m[r] - mine);
+          m[r] = mine;
+          if (e == hf) l[i] *= f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) o[r][c] *= f;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRows / 2; ++i) {
+      const float p = ex2(z[i] - (hf ? m[2 * i + 1] : m[2 * i]));
+      l[i] += p;
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(ps + (key * kRows + 2 * i + hf) * 4), "f"(p) : "memory");
+    }
+    __syncwarp();
+    const int keys = min(kWarpKeys, u.limit - base);                      // rows behind the last visible one may hold anything
+    for (int k = 0; k < keys; ++k) {
+      float4 v;
+      if (kFp4) {
+        const uint32_t two = lds_u16(stage + 1024 + piece4(k, lane >> 3) + 2 * (lane & 7));
+        const float f = scale_to_float(lds_u8(stage + 2176 + 8 * k + (lane >> 2)));
+        const float2 x = __half22float2(fp4x2_to_half2(two & 255u)), y = __half22float2(fp4x2_to_half2(two >> 8));
+        v = make_float4(f * x.x, f * x.y, f * y.x, f * y.y);
+      } else {
+        v = lds_f4(stage + 8192 + piece32(k, lane));
+      }
+      const float4 pa = lds_f4(ps + k * kRows * 4), pb = lds_f4(ps + k * kRows * 4 + 16);
+      const float p[kRows] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        o[r][0] = fmaf(p[r], v.x, o[r][0]);
+        o[r][1] = fmaf(p[r], v.y, o[r][1]);
+        o[r][2] = fmaf(p[r], v.z, o[r][2]);
+        o[r][3] = fmaf(p[r], v.w, o[r][3]);
+      }
+    }
+    __syncwarp();
+  }
+
+  __device__ __forceinline__ void flush(float* buf, float2* ml, int, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kRows / 2; ++i) {
+      float sum = l[i];
+#pragma unroll
+      for (int x = 2; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      if (lane < 2) ml[2 * i + lane] = make_float2(lane ? m[2 * i + 1] : m[2 * i], sum);
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) *reinterpret_cast<float4*>(buf + r * kPadRow + 4 * lane) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+  }
+  __device__ __forceinline__ static int channel(int p) { return p; }
+};
+
+// ---- the kernel -----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void store2(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
+__device__ __forceinline__ void store2(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
+
+// Positions 4 lane .. 4 lane + 3 of row r of the unit, weights summing to `sum` against the maximum `top`.
+template <class E>
+__device__ __forceinline__ void write_row(const Attend& a, const Unit& u, int r, float4 acc, float top, float sum, int lane) {
+  const int row = u.row0 + r;
+  if (row >= u.rows) return;
+  const int i = row / a.group, h = u.h * a.group + row - i * a.group;
+  const int64_t at = (int64_t)(a.t.cu[u.b] + i) * a.n_q_heads + h;
+  const float f = sum == 0.f ? 0.f : (a.pg.fp4 ? a.pg.v_scale : 1.f) / sum;
+  typename E::T* out = (typename E::T*)a.out + at * kHeadDim;
+  store2(out + E::channel(4 * lane), acc.x * f, acc.y * f);
+  store2(out + E::channel(4 * lane + 2), acc.z * f, acc.w * f);
+  if (a.lse != nullptr && lane == 0) a.lse[at] = sum == 0.f ? -CUDART_INF_F : (top - E::kLift + log2f(sum)) * 0.69314718f;
+}
+
+template <class E>
+__global__ void __launch_bounds__(E::kWarps * 32, E::kCtas)
+paged_attend_kernel(const __grid_constant__ Attend a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int kThreads = E::kWarps * 32, kBufRow = 8 * kPadRow;
+  unsigned char* const stages = smem;                                               // [kWarps][kStages][kStageBytes]
+  float* const buf = reinterpret_cast<float*>(smem + E::kWarps * E::kStages * E::kStageBytes);   // [kWarps][8][kPadRow]
+  float2* const ml = reinterpret_cast<float2*>(buf + E::kWarps * kBufRow);          // [kWarps][8]
+  unsigned char* const extra = reinterpret_cast<unsigned char*>(ml + E::kWarps * 8);
+  __shared__ Shape shape;
+  __shared__ int last_here;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_trigger();
+
+  // tiles before each sequence
+  if (warp == 0) {
+    int64_t run = 0;
+    for (int b0 = 0; b0 < a.t.batch; b0 += 32) {
+      int units = 0;
+      const int b = b0 + lane, tiles = b < a.t.batch ? tiles_of<E>(a, b, &units) : 0;
+      if (blockIdx.x == 0 && tiles > 0 && (int64_t)a.pg.len[b] + (a.t.cu[b + 1] - a.t.cu[b]) > (int64_t)a.pg.table_stride << a.pg.page_shift)
+        atomicOr(a.status, kStatusBadPage);
+      int64_t x = (int64_t)tiles * units;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      if (b < a.t.batch) shape.before[b + 1] = run + x;
+      run += __shfl_sync(0xffffffffu, x, 31);
+    }
+    if (lane == 0) shape.before[0] = 0;
+  }
+  __syncthreads();
+  const int64_t total = shape.before[a.t.batch];
+  const int64_t ctas = min((int64_t)gridDim.x, total);
+  if (blockIdx.x >= ctas) return;
+  const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+
+  Cursor c;
+  {
+    int lo = 0, hi = a.t.batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (shape.before[mid] <= begin) lo = mid; else hi = mid - 1;
+    }
+    c.pos = begin;
+    c.end = end;
+    c.b = lo;
+    c.tiles = tiles_of<E>(a, lo, &c.units);
+    const int64_t in = begin - shape.before[lo];
+    c.unit = (int)(in / c.tiles);
+    c.tile = (int)(in - (int64_t)c.unit * c.tiles);
+  }
+  Cursor p = c;                                                           // the tile whose rows are copied next
+  Unit pu = unit_of<E>(a, p);
+  int p_unit = p.unit, p_b = p.b, page = 0;
+  uint32_t bad = 0;                                                       // stages whose page does not exist
+  const uint32_t mine = smem_u32(stages) + warp * E::kStages * E::kStageBytes;
+  auto look_up = [&] {                                                    // the page of tile p (one tile ahead of its use)
+    if (p.pos >= p.end) return;
+    if (p.unit != p_unit || p.b != p_b) {
+      pu = unit_of<E>(a, p);
+      p_unit = p.unit;
+      p_b = p.b;
+    }
+    const int base = p.tile * E::kTile + warp * kWarpKeys;
+    if (base < pu.limit) page = __ldg(a.pg.table + pu.table + (base >> a.pg.page_shift));
+  };
+  auto produce = [&](int slot) {
+    if (p.pos < p.end) {
+      const int base = p.tile * E::kTile + warp * kWarpKeys;
+      bad &= ~(1u << slot);
+      if (base < pu.limit) {
+        if ((unsigned)page < (unsigned)a.pg.n_pages) {
+          E::issue(a, mine + slot * E::kStageBytes,
+                   page * a.pg.page_stride + pu.h * a.pg.head_stride + (int64_t)(base & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride, lane);
+        } else {
+          bad |= 1u << slot;
+          if (lane == 0) atomicOr(a.status, kStatusBadPage);
+        }
+      }
+      advance<E>(a, p);
+      look_up();
+    }
+    ptx::cp_async_commit();
+  };
+  look_up();
+  for (int st = 0; st < E::kStages - 1; ++st) produce(st);
+
+  E e;
+  Unit u = unit_of<E>(a, c);
+  e.begin(a, u, extra, warp, lane);
+  int slot = 0;
+  for (; c.pos < c.end;) {
+    int ahead = slot + E::kStages - 1;
+    if (ahead >= E::kStages) ahead -= E::kStages;
+    produce(ahead);
+    ptx::cp_async_wait<E::kStages - 1>();
+    __syncwarp();
+    const int base = c.tile * E::kTile + warp * kWarpKeys;
+    if (base < u.limit && !((bad >> slot) & 1u)) e.step(a, u, mine + slot * E::kStageBytes, base, base + kWarpKeys <= u.full, extra, warp, lane);
+    __syncwarp();
+    if (++slot == E::kStages) slot = 0;
+    const int64_t unit_begin = c.pos - c.tile, unit_end = unit_begin + c.tiles;
+    if (c.tile + 1 < c.tiles && c.pos + 1 < c.end) {
+      advance<E>(a, c);
+      continue;
+    }
+    // ---- the run leaves this unit
+    const bool alone = unit_begin >= begin && unit_end <= end;
+    const int64_t c0 = ((unit_begin + 1) * ctas - 1) / total, c1 = (unit_end * ctas - 1) / total;
+    constexpr int64_t kSlotFloats = (int64_t)kMaxRows * kPartRow;
+    float* const part = a.part + (2 * (int64_t)blockIdx.x + (unit_begin > begin ? 1 : 0)) * kSlotFloats;
+    for (int nt = 0; nt < E::kNT; ++nt) {
+      __syncthreads();
+      e.flush(buf + warp * kBufRow, ml + warp * 8, nt, lane);
+      __syncthreads();
+      for (int r = warp; r < 8; r += E::kWarps) {
+        float top = kLowest, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < E::kWarps; ++w) top = fmaxf(top, ml[w * 8 + r].x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < E::kWarps; ++w) {
+          const float f = ex2(ml[w * 8 + r].x - top);
+          const float4 x = *reinterpret_cast<const float4*>(buf + w * kBufRow + r * kPadRow + 4 * lane);
+          sum = fmaf(f, ml[w * 8 + r].y, sum);
+          acc = make_float4(fmaf(f, x.x, acc.x), fmaf(f, x.y, acc.y), fmaf(f, x.z, acc.z), fmaf(f, x.w, acc.w));
+        }
+        if (alone) {
+          write_row<E>(a, u, 8 * nt + r, acc, top, sum, lane);
+        } else {
+          float* to = part + (8 * nt + r) * kPartRow;
+          __stcg(reinterpret_cast<float2*>(to + 4 * lane), make_float2(acc.x, acc.y));
+          __stcg(reinterpret_cast<float2*>(to + 4 * lane + 2), make_float2(acc.z, acc.w));
+          if (lane == 0) __stcg(reinterpret_cast<float2*>(to + kHeadDim), make_float2(top, sum));
+        }
+      }
+    }
+    if (!alone) {
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) last_here = atomicAdd(a.sync + c0, 1u) == (uint32_t)(c1 - c0);
+      __syncthreads();
+      if (last_here) {
+        __threadfence();
+        const bool inside = unit_begin > total * c0 / ctas;               // (the first CTA's part: behind another one of its own)
+        const float* first = a.part + (2 * c0 + (inside ? 1 : 0)) * kSlotFloats;
+        const int n = (int)(c1 - c0) + 1;
+        for (int r = warp; r < E::kRows; r += E::kWarps) {
+          auto from = [&](int x) { return (x == 0 ? first : a.part + 2 * (c0 + x) * kSlotFloats) + r * kPartRow; };
+          float top = kLowest;
+          for (int x = lane; x < n; x += 32) top = fmaxf(top, __ldcg(from(x) + kHeadDim));
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          float sum = 0.f;
+#pragma unroll 8
+          for (int x = 0; x < n; ++x) {
+            const float* at = from(x);
+            const float2 mx = __ldcg(reinterpret_cast<const float2*>(at + kHeadDim)), lo = __ldcg(reinterpret_cast<const float2*>(at + 4 * lane)),
+                         hi = __ldcg(reinterpret_cast<const float2*>(at + 4 * lane + 2));
+            const float f = ex2(mx.x - top);
+            sum = fmaf(f, mx.y, sum);
+            acc = make_float4(fmaf(f, lo.x, acc.x), fmaf(f, lo.y, acc.y), fmaf(f, hi.x, acc.z), fmaf(f, hi.y, acc.w));
+          }
+          write_row<E>(a, u, r, acc, top, sum, lane);
+        }
+        if (threadIdx.x == 0) a.sync[c0] = 0u;
+      }
+    }
+    advance<E>(a, c);
+    if (c.pos < c.end) {
+      u = unit_of<E>(a, c);
+      __syncthreads();
+      e.begin(a, u, extra, warp, lane);
+    }
+  }
+  ptx::cp_async_wait<0>();
+}
+
+template <class E>
+cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
+  constexpr int smem = E::kWarps * (E::kStages * E::kStageBytes + 8 * kPadRow * 4 + 64) + E::kExtra;
+  cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  // no more CTAs than there can be tiles
+  int64_t most = 0;
+  const int64_t tiles = (((int64_t)a.pg.table_stride << a.pg.page_shift) + E::kTile - 1) / E::kTile;
+  for (int b = 0; b < a.t.batch; ++b) most += (int64_t)a.n_kv_heads * (((int64_t)(a.t.cu[b + 1] - a.t.cu[b]) * a.group + E::kRows - 1) / E::kRows) * tiles;
+  const int64_t grid = (int64_t)n_sm * E::kCtas;
+  return launch_pdl(paged_attend_kernel<E>, dim3((unsigned)(most < grid ? most : grid)), dim3(E::kWarps * 32), smem, s, 1, a);
+}
+
+}  // namespace
+
+size_t attend_part_floats(int n_sm) { return (size_t)2 * n_sm * kMaxCtasPerSm * kMaxRows * kPartRow; }
+size_t attend_sync_words(int n_sm) { return (size_t)n_sm * kMaxCtasPerSm; }
+
+cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t, const Dims& dm, const void* q, int64_t q_stride, float softcap, void* out,
+                                float* lse, float* part, uint32_t* sync, int n_sm, int* status, cudaStream_t s, LaunchLog* log) {
+  Attend a = {pg, t, q, q_stride, out, lse, part, sync, status, dm.n_q_heads, dm.n_kv_heads, dm.group, dm.scale_log2e, softcap};
+  int rows = 0;
+  for (int b = 0; b < t.batch; ++b) rows = max(rows, (t.cu[b + 1] - t.cu[b]) * dm.group);
+  log->begin(kKindPagedAttend, s);
+  cudaError_t e;
+  if (dtype == DAPQ_F32) e = pg.fp4 ? go<FloatEngine<true>>(a, n_sm, s) : go<FloatEngine<false>>(a, n_sm, s);
+  else if (rows <= 8) e = pg.fp4 ? go<TensorEngine<true, 1>>(a, n_sm, s) : go<TensorEngine<false, 1>>(a, n_sm, s);
+  else e = pg.fp4 ? go<TensorEngine<true, 2>>(a, n_sm, s) : go<TensorEngine<false, 2>>(a, n_sm, s);
+  log->end(s);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace dapq

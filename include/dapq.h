@@ -315,7 +315,7 @@ typedef struct {
   void* v_scales;
   int64_t page_stride;            /* channels between pages, heads, rows of K and of V alike; the codes lie at stride / 2 */
   int64_t head_stride;            /* bytes, the scales at stride / 16.  Multiples of 16 bytes; of 128 channels for */
-  int64_t row_stride;             /* DAPQ_CACHE_FP4.  row_stride >= d             */
+  int64_t row_stride;             /* DAPQ_CACHE_FP4.  row_stride: d .. 2^24       */
   const int32_t* page_table;      /* device [B][table_stride]                     */
   const int32_t* cache_len;       /* device [B]                                   */
   int32_t table_stride;           /* pages that a row of the table has room for   */

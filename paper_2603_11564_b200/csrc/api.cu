@@ -1073,6 +1073,7 @@ dapq_status dapq_evict_host(dapq_ctx* ctx, const void* q_pre_host, const dapq_ca
 // ---- the paged cache --------------------------------------------------------------------------------------------------
 namespace {
 
+constexpr int64_t kMaxRowStride = 1 << 24;         // 16 rows of fp32 within 2^31 bytes
 constexpr int64_t kMaxPagedRows = 0x7ff00000LL;    // of a sequence: row numbers stay in 32 bits
 
 dapq_status check_paged(dapq_ctx* ctx, const char* who, const dapq_paged_cache* pc, bool need_len, PagedDev* out) {
@@ -1089,6 +1090,7 @@ dapq_status check_paged(dapq_ctx* ctx, const char* who, const dapq_paged_cache* 
     return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: page_rows must be a power of two in 16 .. 1024 (got %d)", who, pc->page_rows);
   if ((int64_t)pc->table_stride * pc->page_rows > kMaxPagedRows)
     return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: a sequence's table has room for more than %lld rows", who, (long long)kMaxPagedRows);
+  if (pc->row_stride > kMaxRowStride) return fail(ctx, DAPQ_ERR_UNSUPPORTED, "%s: row_stride must be at most %lld", who, (long long)kMaxRowStride);
   if (pc->row_stride < kHeadDim || pc->head_stride < 0 || pc->page_stride < 0)
     return fail(ctx, DAPQ_ERR_INVALID_ARG, "%s: row_stride must be >= head_dim, head_stride and page_stride >= 0", who);
   const int64_t unit = fp4 ? kHeadDim : 16 / ctx->elem_bytes;

@@ -1,8 +1,6 @@
 // The paged cache: geometry, page lookup and the 4-bit format (include/dapq.h states both).
 #pragma once
 #include <cuda_fp16.h>
-#include <cuda_fp4.h>
-#include <cuda_fp8.h>
 
 #include "dapq_internal.cuh"
 
@@ -57,14 +55,38 @@ __device__ __forceinline__ int64_t paged_row(const PagedDev& pg, int b, int64_t 
   return page * pg.page_stride + head * pg.head_stride + (row & ((1 << pg.page_shift) - 1)) * pg.row_stride;
 }
 
-// Two codes of a byte as fp16 (exact).
-__device__ __forceinline__ __half2 fp4x2_to_half2(uint32_t byte) {
-  return __half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)byte, __NV_E2M1));
+// ---- the 4-bit format in registers ------------------------------------------------------------------------------------
+// The eight codes of a word as fp16, channels 2 i, 2 i + 1 in h[i] (exact).
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t* h) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
 }
-// Two e4m3 scales as fp16 (exact).
-__device__ __forceinline__ __half2 scales_to_half2(uint32_t two) {
-  return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3));
+// Two e4m3 scales (the low bytes of x) as fp16 (exact).
+__device__ __forceinline__ uint32_t scales_to_half(uint32_t x) {
+  uint32_t y;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"((uint16_t)x));
+  return y;
 }
-__device__ __forceinline__ float scale_to_float(uint32_t one) { return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)one, __NV_E4M3))); }
+// A scale as fp32.
+__device__ __forceinline__ float scale_to_float(uint32_t one) {
+  return one == 0x7fu ? __uint_as_float(0x7fc00000u) : __half2float(__ushort_as_half((unsigned short)(one << 7))) * 256.f;
+}
+// The nearest e4m3 to s >= 0 (at most 448), ties to even: its bits, and its value in *value.
+__device__ __forceinline__ uint32_t scale_bits(float s, float* value) {
+  const float low = s + 24576.f;                                   // (below 2^-6: multiples of 2^-9, the last bit of 1.5 * 2^14)
+  const uint32_t u = (__float_as_uint(s) + 0x7ffffu + ((__float_as_uint(s) >> 20) & 1u)) >> 20;
+  const bool tiny = s < 0.015625f;
+  *value = tiny ? low - 24576.f : __uint_as_float(u << 20);
+  return tiny ? __float_as_uint(low) & 15u : u - (120u << 3);
+}
+// The nearest e2m1 to y in 0 .. 6, ties to even: a sum whose last bit is the step of y's range leaves the code in its last three.
+__device__ __forceinline__ uint32_t code_bits(float y) {
+  return __float_as_uint(y + (y < 2.f ? 6291456.f : y < 4.f ? 12582914.f : 25165832.f)) & 7u;
+}
 
 }  // namespace dapq

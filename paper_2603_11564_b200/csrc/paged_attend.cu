@@ -27,7 +27,8 @@ using ptx::smem_u32;
 constexpr int kWarpKeys = 16;
 constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
 constexpr int kPadRow = 132;                         // floats of a row of the warps' partial outputs (conflict-free, see flush)
-constexpr int kMaxRows = 16, kPartRow = kHeadDim + 2, kMaxCtasPerSm = 2;
+constexpr int kMaxRows = 16, kMaxCtasPerSm = 2;
+constexpr int kSlotFloats = kMaxRows * (kHeadDim + 2);   // a partial result: [rows][128] outputs, [rows] maxima and sums
 
 struct Attend {
   PagedDev pg;
@@ -54,6 +55,11 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 __device__ __forceinline__ float4 lds_f4(uint32_t a) {
   float4 v;
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
 __device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
@@ -91,64 +97,60 @@ struct Unit {
   int rows;                // rows of the sequence
   int held, limit;         // rows held before the step, end of the rows that any of the tile's queries sees
   int full;                // end of the rows that all of them see
-  int64_t table;           // its row of the page table
 };
 
-// Walks the CTA's run of tiles.
-struct Cursor {
-  int64_t pos, end;
-  int b, unit, tile, tiles, units;
-};
-
-// The geometry that every CTA works out for itself, in shared memory.
-struct Shape {
-  int64_t before[kMaxBatch + 1];                     // tiles of the sequences before
-};
-
+// Tiles of a sequence's units, and their number.
 template <class E>
-__device__ __forceinline__ int tiles_of(const Attend& a, int b, int* units) {
-  const int n = a.t.cu[b + 1] - a.t.cu[b], held = a.pg.len[b];
+__device__ __forceinline__ int tiles_of(const Attend& a, int b, int held, int* units) {
+  const int n = a.t.cu[b + 1] - a.t.cu[b];
   *units = a.n_kv_heads * ((n * a.group + E::kRows - 1) / E::kRows);
   const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift, rows = held < 0 ? 0 : min((int64_t)held + n, room);
   return n == 0 ? 0 : max(1, (int)((rows + E::kTile - 1) / E::kTile));
 }
 
-template <class E>
-__device__ __forceinline__ void enter(const Attend& a, Cursor& c) {     // c.b is set; skips sequences without tiles
-  while (c.b < a.t.batch) {
-    c.tiles = tiles_of<E>(a, c.b, &c.units);
-    if (c.tiles > 0) break;
-    ++c.b;
-  }
-}
-template <class E>
-__device__ __forceinline__ void advance(const Attend& a, Cursor& c) {
-  ++c.pos;
-  if (++c.tile == c.tiles) {
-    c.tile = 0;
-    if (++c.unit == c.units && c.pos < c.end) {
-      c.unit = 0;
-      ++c.b;
-      enter<E>(a, c);
-    }
-  }
-}
-template <class E>
-__device__ __forceinline__ Unit unit_of(const Attend& a, const Cursor& c) {
+// A part of a CTA's run of tiles that lies in one unit.
+struct Part {
+  int64_t begin, end, unit_begin;                    // tiles of the call: [begin, end) of the unit's [unit_begin, unit_begin + tiles)
+  int tiles, unit;                                   // of the sequence u.b
   Unit u;
-  u.b = c.b;
-  const int n = a.t.cu[c.b + 1] - a.t.cu[c.b];
+};
+
+template <class E>
+__device__ __forceinline__ void place(const Attend& a, Part& p, int b, int unit, int64_t unit_begin, int64_t begin, int64_t run_end) {
+  const int n = a.t.cu[b + 1] - a.t.cu[b], held = a.pg.len[b];
+  int units;
+  p.tiles = tiles_of<E>(a, b, held, &units);
+  p.unit = unit;
+  p.unit_begin = unit_begin;
+  p.begin = begin;
+  p.end = min(run_end, unit_begin + p.tiles);
+  Unit& u = p.u;
+  u.b = b;
   u.rows = n * a.group;
-  const int tiles = (u.rows + E::kRows - 1) / E::kRows;
-  u.h = c.unit / tiles;
-  u.row0 = (c.unit - u.h * tiles) * E::kRows;
-  u.held = a.pg.len[c.b];
+  const int row_tiles = units / a.n_kv_heads;
+  u.h = unit / row_tiles;
+  u.row0 = (unit - u.h * row_tiles) * E::kRows;
+  u.held = held;
   const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift;
   const int first = u.row0 / a.group, last = min((u.row0 + E::kRows - 1) / a.group, n - 1);
-  u.limit = u.held < 0 ? 0 : (int)min((int64_t)u.held + last + 1, room);
-  u.full = u.held < 0 ? 0 : (int)min((int64_t)u.held + first + 1, room);
-  u.table = (int64_t)c.b * a.pg.table_stride;
-  return u;
+  u.limit = held < 0 ? 0 : (int)min((int64_t)held + last + 1, room);
+  u.full = held < 0 ? 0 : (int)min((int64_t)held + first + 1, room);
+}
+// The part of the run behind p, if there is one.
+template <class E>
+__device__ __forceinline__ bool next(const Attend& a, Part& p, const int64_t* before, int64_t run_end) {
+  if (p.end >= run_end) {
+    p.begin = p.end;
+    return false;
+  }
+  const int64_t at = p.end;                          // (the part ended with its unit)
+  int b = p.u.b, unit = p.unit + 1;
+  if (at >= before[b + 1]) {
+    unit = 0;
+    do ++b; while (before[b + 1] <= at);
+  }
+  place<E>(a, p, b, unit, at, at, run_end);
+  return true;
 }
 // Rows that query row r of the unit sees.
 __device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
@@ -166,7 +168,7 @@ __device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
 template <bool kFp4, int kTiles>
 struct TensorEngine {
   static constexpr int kNT = kTiles;
-  static constexpr int kWarps = 8, kTile = kWarps * kWarpKeys, kRows = 8 * kNT, kCtas = kFp4 && kNT == 1 ? 2 : 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kWarps = kFp4 && kNT == 1 ? 16 : 8, kTile = kWarps * kWarpKeys, kRows = 8 * kNT, kCtas = 1, kStages = kFp4 ? 4 : 3, kMinRun = 4, kByteShift = kFp4 ? -1 : 1;
   static constexpr int kStageBytes = kFp4 ? kWarpKeys * 144 : kWarpKeys * 512;
   static constexpr int kExtra = 0;
   static constexpr float kLift = kFp4 ? 11.f : 0.f;
@@ -181,26 +183,40 @@ struct TensorEngine {
   __device__ __forceinline__ static int piece4(int r, int c) { return r * 64 + ((c ^ (((r >> 1) & 1) << 1)) << 4); }
   __device__ __forceinline__ static int piece16(int r, int c) { return r * 256 + ((c ^ (((r & 3) << 1) | ((r >> 2) & 1))) << 4); }
 
-  // Rows of the stage: off is the channel offset of the tile's first row.
-  __device__ __forceinline__ static void issue(const Attend& a, uint32_t stage, int64_t off, int lane) {
-    const int64_t step = a.pg.row_stride;
-    if (kFp4) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = (lane >> 2) + 8 * j, c = lane & 3;
-        const int64_t at = (off + r * step) / 2 + c * 16;
-        ptx::cp_async16(stage + piece4(r, c), a.pg.k + at);
-        ptx::cp_async16(stage + 1024 + piece4(r, c), a.pg.v + at);
+  // A lane's pieces of a tile of 16 rows: byte offsets from the tile's first row in memory (code bytes in 4 bits) and in the stage.
+  struct Lane {
+    uint32_t from, to, rows, scale_from, scale_to;
+    bool k_scale;
+    __device__ __forceinline__ Lane(const Attend& a, int lane) {
+      if (kFp4) {
+        rows = (uint32_t)(a.pg.row_stride / 2);
+        from = (lane >> 2) * rows + (lane & 3) * 16;
+        to = piece4(lane >> 2, lane & 3);
+        scale_from = (lane & 15) * (rows >> 3);
+        scale_to = 2048 + 8 * lane;
+        k_scale = lane < 16;
+      } else {
+        rows = (uint32_t)(a.pg.row_stride * 2);
+        from = (lane >> 4) * rows + (lane & 15) * 16;
       }
-      const int r = lane & 15;
-      cp_async8(stage + 2048 + 8 * lane, (lane < 16 ? a.pg.k_scales : a.pg.v_scales) + (off + r * step) / 16);
+    }
+  };
+  // off: the first row's byte offset (code bytes).
+  __device__ __forceinline__ static void issue(const Attend& a, const Lane& ln, uint32_t stage, int64_t off, int lane) {
+    const char *k = a.pg.k + off + ln.from, *v = a.pg.v + off + ln.from;
+    if (kFp4) {
+      ptx::cp_async16(stage + ln.to, k);
+      ptx::cp_async16(stage + ln.to + 1024, v);
+      ptx::cp_async16(stage + ln.to + 512, k + 8 * ln.rows);               // (rows r and r + 8 are swizzled alike)
+      ptx::cp_async16(stage + ln.to + 1536, v + 8 * ln.rows);
+      cp_async8(stage + ln.scale_to, (ln.k_scale ? a.pg.k_scales : a.pg.v_scales) + (off >> 3) + ln.scale_from);
     } else {
+      const int r0 = lane >> 4, c = lane & 15;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int r = (lane >> 4) + 2 * j, c = lane & 15;
-        const int64_t at = (off + r * step) * 2 + c * 16;
-        ptx::cp_async16(stage + piece16(r, c), a.pg.k + at);
-        ptx::cp_async16(stage + 4096 + piece16(r, c), a.pg.v + at);
+        const uint32_t to = piece16(r0 + 2 * j, c);
+        ptx::cp_async16(stage + to, k + 2 * j * ln.rows);
+        ptx::cp_async16(stage + 4096 + to, v + 2 * j * ln.rows);
       }
     }
   }
@@ -250,8 +266,9 @@ struct TensorEngine {
     }
   }
 
-  // Keys base .. base + 15 of the sequence; whole: all of the tile's queries see all of them.
-  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, bool whole, unsigned char*, int, int lane) {
+  // Keys base .. base + 15 of the sequence; whole: all of the unit's queries see all of them.
+  template <bool whole>
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char*, int, int lane) {
     const int g = lane >> 2, t = lane & 3, rk = key_of(g);
     float s[kNT][4];
 #pragma unroll
@@ -260,17 +277,20 @@ struct TensorEngine {
       for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
     if (kFp4) {
       const uint4 ka = ptx::lds128(stage + piece4(rk, t)), kb = ptx::lds128(stage + piece4(rk + 8, t));
-      const __half2 sa = scales_to_half2(lds_u16(stage + 2048 + 8 * rk + 2 * t)), sb = scales_to_half2(lds_u16(stage + 2048 + 8 * rk + 64 + 2 * t));
+      const uint32_t sa = scales_to_half(lds_u16(stage + 2048 + 8 * rk + 2 * t)), sb = scales_to_half(lds_u16(stage + 2048 + 8 * rk + 64 + 2 * t));
       const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const __half2 fa = w < 2 ? __low2half2(sa) : __high2half2(sa), fb = w < 2 ? __low2half2(sb) : __high2half2(sb);
+        const __half2 fa = w < 2 ? __low2half2(halves(sa)) : __high2half2(halves(sa)), fb = w < 2 ? __low2half2(halves(sb)) : __high2half2(halves(sb));
+        uint32_t ha[4], hb[4];
+        codes_to_half(wa[w], ha);
+        codes_to_half(wb[w], hb);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const uint32_t a0 = bits(__hmul2(fp4x2_to_half2((wa[w] >> (16 * p)) & 255u), fa)), a2 = bits(__hmul2(fp4x2_to_half2((wa[w] >> (16 * p + 8)) & 255u), fa));
-          const uint32_t a1 = bits(__hmul2(fp4x2_to_half2((wb[w] >> (16 * p)) & 255u), fb)), a3 = bits(__hmul2(fp4x2_to_half2((wb[w] >> (16 * p + 8)) & 255u), fb));
+        for (int p = 0; p < 4; p += 2) {
+          const uint32_t a0 = bits(__hmul2(halves(ha[p]), fa)), a2 = bits(__hmul2(halves(ha[p + 1]), fa));
+          const uint32_t a1 = bits(__hmul2(halves(hb[p]), fb)), a3 = bits(__hmul2(halves(hb[p + 1]), fb));
 #pragma unroll
-          for (int nt = 0; nt < kNT; ++nt) mma<true>(s[nt], a0, a1, a2, a3, q[nt][4 * w + 2 * p], q[nt][4 * w + 2 * p + 1]);
+          for (int nt = 0; nt < kNT; ++nt) mma<true>(s[nt], a0, a1, a2, a3, q[nt][4 * w + p], q[nt][4 * w + p + 1]);
         }
       }
     } else {
@@ -349,16 +369,19 @@ struct TensorEngine {
         sc[i] = lds_u8(stage + 2176 + 8 * rv[i] + g);
         if (!whole && base + rv[i] >= u.limit) sc[i] = 0;
       }
-      const __half2 f01 = scales_to_half2(sc[0] | (sc[1] << 8)), f23 = scales_to_half2(sc[2] | (sc[3] << 8));
+      const __half2 f01 = halves(scales_to_half(sc[0] | (sc[1] << 8))), f23 = halves(scales_to_half(sc[2] | (sc[3] << 8)));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        uint32_t x[4];
+      for (int x = 0; x < 2; ++x) {
+        uint32_t h[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = bits(fp4x2_to_half2((w[i][j >> 2] >> (8 * (j & 3))) & 255u));
-        const uint32_t a0 = bits(__hmul2(halves(__byte_perm(x[0], x[1], 0x5410)), f01)), a1 = bits(__hmul2(halves(__byte_perm(x[0], x[1], 0x7632)), f01));
-        const uint32_t a2 = bits(__hmul2(halves(__byte_perm(x[2], x[3], 0x5410)), f23)), a3 = bits(__hmul2(halves(__byte_perm(x[2], x[3], 0x7632)), f23));
+        for (int i = 0; i < 4; ++i) codes_to_half(w[i][x], h[i]);
 #pragma unroll
-        for (int nt = 0; nt < kNT; ++nt) mma<true>(o[nt][j], a0, a1, a2, a3, p0[nt], p1[nt]);
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t a0 = bits(__hmul2(halves(__byte_perm(h[0][j], h[1][j], 0x5410)), f01)), a1 = bits(__hmul2(halves(__byte_perm(h[0][j], h[1][j], 0x7632)), f01));
+          const uint32_t a2 = bits(__hmul2(halves(__byte_perm(h[2][j], h[3][j], 0x5410)), f23)), a3 = bits(__hmul2(halves(__byte_perm(h[2][j], h[3][j], 0x7632)), f23));
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) mma<true>(o[nt][4 * x + j], a0, a1, a2, a3, p0[nt], p1[nt]);
+        }
       }
     } else {
 #pragma unroll
@@ -410,7 +433,7 @@ struct TensorEngine {
 // outputs, queries and weights broadcast from shared memory.
 template <bool kFp4>
 struct FloatEngine {
-  static constexpr int kWarps = 4, kTile = kWarps * kWarpKeys, kRows = 8, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kWarps = 4, kTile = kWarps * kWarpKeys, kRows = 8, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
   static constexpr int kStageBytes = kFp4 ? kWarpKeys * 144 : kWarpKeys * 1024;
   static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = kWarpKeys * kRows * 4;
   static constexpr int kExtra = kQBytes + kWarps * kPBytes;
@@ -423,15 +446,23 @@ struct FloatEngine {
   __device__ __forceinline__ static int piece4(int r, int c) { return TensorEngine<true, 1>::piece4(r, c); }
   __device__ __forceinline__ static int piece32(int r, int c) { return r * 512 + ((c ^ ((r & 3) << 1)) << 4); }
 
-  __device__ __forceinline__ static void issue(const Attend& a, uint32_t stage, int64_t off, int lane) {
+  struct Lane : TensorEngine<true, 1>::Lane {
+    __device__ __forceinline__ Lane(const Attend& a, int lane) : TensorEngine<true, 1>::Lane(a, lane) {
+      if (!kFp4) {
+        this->rows = (uint32_t)(a.pg.row_stride * 4);
+        this->from = lane * 16;
+      }
+    }
+  };
+  __device__ __forceinline__ static void issue(const Attend& a, const Lane& ln, uint32_t stage, int64_t off, int lane) {
     if (kFp4) {
-      TensorEngine<true, 1>::issue(a, stage, off, lane);
+      TensorEngine<true, 1>::issue(a, ln, stage, off, lane);
     } else {
+      const char *k = a.pg.k + off + ln.from, *v = a.pg.v + off + ln.from;
 #pragma unroll
       for (int r = 0; r < kWarpKeys; ++r) {
-        const int64_t at = (off + r * a.pg.row_stride) * 4 + lane * 16;
-        ptx::cp_async16(stage + piece32(r, lane), a.pg.k + at);
-        ptx::cp_async16(stage + 8192 + piece32(r, lane), a.pg.v + at);
+        ptx::cp_async16(stage + piece32(r, lane), k + r * ln.rows);
+        ptx::cp_async16(stage + 8192 + piece32(r, lane), v + r * ln.rows);
       }
     }
   }
@@ -455,7 +486,8 @@ struct FloatEngine {
     for (int r = 0; r < kRows / 2; ++r) l[r] = 0.f;
   }
 
-  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, bool whole, unsigned char* extra, int warp, int lane) {
+  template <bool whole>
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char* extra, int warp, int lane) {
     const int key = lane >> 1, hf = lane & 1;
     const uint32_t qs = smem_u32(extra), ps = qs + kQBytes + warp * kPBytes;
     float s[kRows];
@@ -467,13 +499,17 @@ struct FloatEngine {
         const uint2 w = lds64(stage + piece4(key, 2 * hf + (p >> 1)) + 8 * (p & 1));
         const float f = scale_to_float(lds_u8(stage + 2048 + 8 * key + 4 * hf + p));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {                                     // four channels
-          const uint32_t two = (c < 2 ? w.x : w.y) >> (16 * (c & 1));
-          const float2 x = __half22float2(fp4x2_to_half2(two & 255u)), y = __half22float2(fp4x2_to_half2((two >> 8) & 255u));
+        for (int c = 0; c < 2; ++c) {                                     // eight channels
+          uint32_t h[4];
+          codes_to_half(c ? w.y : w.x, h);
 #pragma unroll
-          for (int r = 0; r < kRows; ++r) {
-            const float4 qv = lds_f4(qs + r * kHeadDim * 4 + (64 * hf + 16 * p + 4 * c) * 4);
-            s[r] = fmaf(f * x.x, qv.x, fmaf(f * x.y, qv.y, fmaf(f * y.x, qv.z, fmaf(f * y.y, qv.w, s[r]))));
+          for (int e = 0; e < 4; e += 2) {
+            const float2 x = __half22float2(halves(h[e])), y = __half22float2(halves(h[e + 1]));
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+              const float4 qv = lds_f4(qs + r * kHeadDim * 4 + (64 * hf + 16 * p + 8 * c + 2 * e) * 4);
+              s[r] = fmaf(f * x.x, qv.x, fmaf(f * x.y, qv.y, fmaf(f * y.x, qv.z, fmaf(f * y.y, qv.w, s[r]))));
+            }
           }
         }
       }
@@ -527,9 +563,10 @@ struct FloatEngine {
     for (int k = 0; k < keys; ++k) {
       float4 v;
       if (kFp4) {
-        const uint32_t two = lds_u16(stage + 1024 + piece4(k, lane >> 3) + 2 * (lane & 7));
         const float f = scale_to_float(lds_u8(stage + 2176 + 8 * k + (lane >> 2)));
-        const float2 x = __half22float2(fp4x2_to_half2(two & 255u)), y = __half22float2(fp4x2_to_half2(two >> 8));
+        uint32_t h[4];                                                    // (the word that this lane shares with its neighbour)
+        codes_to_half(lds_u32(stage + 1024 + piece4(k, lane >> 3) + 4 * ((lane & 7) >> 1)), h);
+        const float2 x = __half22float2(halves(lane & 1 ? h[2] : h[0])), y = __half22float2(halves(lane & 1 ? h[3] : h[1]));
         v = make_float4(f * x.x, f * x.y, f * y.x, f * y.y);
       } else {
         v = lds_f4(stage + 8192 + piece32(k, lane));
@@ -579,6 +616,42 @@ __device__ __forceinline__ void write_row(const Attend& a, const Unit& u, int r,
   if (a.lse != nullptr && lane == 0) a.lse[at] = sum == 0.f ? -CUDART_INF_F : (top - E::kLift + log2f(sum)) * 0.69314718f;
 }
 
+// Row r of a unit from the partial results of n CTAs, in their order: the first one's at `first`, the x-th one's at others + 2 x slots.  A
+// warp's loads of kBatch of them are in flight together (one after the other they cost 25 us for the 74 of a cache of 128k rows).
+template <class E>
+__device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r, const float* first, const float* others, int n, int lane) {
+  constexpr int kBatch = 8;
+  auto from = [&](int x) { return x == 0 ? first : others + 2 * (int64_t)x * kSlotFloats; };
+  auto stats = [&](int x) { return __ldcg(reinterpret_cast<const float2*>(from(x) + kMaxRows * kHeadDim) + r); };
+  float top = kLowest;
+  for (int x = lane; x < n; x += 32) top = fmaxf(top, stats(x).x);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float sum = 0.f;
+  for (int x0 = 0; x0 < n; x0 += 32) {
+    float weight = 0.f;
+    if (x0 + lane < n) {
+      const float2 mx = stats(x0 + lane);
+      weight = ex2(mx.x - top);
+      sum = fmaf(weight, mx.y, sum);
+    }
+    for (int x1 = x0; x1 < min(x0 + 32, n); x1 += kBatch) {
+      float4 v[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(from(min(x1 + i, n - 1)) + r * kHeadDim) + lane);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float f = __shfl_sync(0xffffffffu, weight, x1 - x0 + i);    // (0 behind the last one)
+        if (x1 + i < n) acc = make_float4(fmaf(f, v[i].x, acc.x), fmaf(f, v[i].y, acc.y), fmaf(f, v[i].z, acc.z), fmaf(f, v[i].w, acc.w));
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  write_row<E>(a, u, r, acc, top, sum, lane);
+}
+
 template <class E>
 __global__ void __launch_bounds__(E::kWarps * 32, E::kCtas)
 paged_attend_kernel(const __grid_constant__ Attend a) {
@@ -588,112 +661,120 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
   float* const buf = reinterpret_cast<float*>(smem + E::kWarps * E::kStages * E::kStageBytes);   // [kWarps][8][kPadRow]
   float2* const ml = reinterpret_cast<float2*>(buf + E::kWarps * kBufRow);          // [kWarps][8]
   unsigned char* const extra = reinterpret_cast<unsigned char*>(ml + E::kWarps * 8);
-  __shared__ Shape shape;
+  __shared__ int64_t before[kMaxBatch + 1];                              // tiles of the sequences before
   __shared__ int last_here;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_trigger();
 
-  // tiles before each sequence
   if (warp == 0) {
     int64_t run = 0;
     for (int b0 = 0; b0 < a.t.batch; b0 += 32) {
-      int units = 0;
-      const int b = b0 + lane, tiles = b < a.t.batch ? tiles_of<E>(a, b, &units) : 0;
-      if (blockIdx.x == 0 && tiles > 0 && (int64_t)a.pg.len[b] + (a.t.cu[b + 1] - a.t.cu[b]) > (int64_t)a.pg.table_stride << a.pg.page_shift)
-        atomicOr(a.status, kStatusBadPage);
+      int units = 0, tiles = 0;
+      const int b = b0 + lane;
+      if (b < a.t.batch) {
+        const int held = a.pg.len[b];
+        tiles = tiles_of<E>(a, b, held, &units);
+        if (blockIdx.x == 0 && tiles > 0 && (int64_t)held + (a.t.cu[b + 1] - a.t.cu[b]) > (int64_t)a.pg.table_stride << a.pg.page_shift)
+          atomicOr(a.status, kStatusBadPage);
+      }
       int64_t x = (int64_t)tiles * units;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
         const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
         if (lane >= d) x += y;
       }
-      if (b < a.t.batch) shape.before[b + 1] = run + x;
+      if (b < a.t.batch) before[b + 1] = run + x;
       run += __shfl_sync(0xffffffffu, x, 31);
     }
-    if (lane == 0) shape.before[0] = 0;
+    if (lane == 0) before[0] = 0;
   }
   __syncthreads();
-  const int64_t total = shape.before[a.t.batch];
-  const int64_t ctas = min((int64_t)gridDim.x, total);
+  // equal runs, of kMinRun tiles at least: below, a CTA more costs more (its part is written, and read by another) than it saves
+  const int64_t total = before[a.t.batch];
+  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / E::kMinRun));
   if (blockIdx.x >= ctas) return;
-  const int64_t begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1) / ctas;
+  const int64_t run_begin = total * blockIdx.x / ctas, run_end = total * (blockIdx.x + 1) / ctas;
 
-  Cursor c;
+  Part c;
   {
-    int lo = 0, hi = a.t.batch - 1;
+    int lo = 0, hi = a.t.batch - 1, units;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (shape.before[mid] <= begin) lo = mid; else hi = mid - 1;
+      if (before[mid] <= run_begin) lo = mid; else hi = mid - 1;
     }
-    c.pos = begin;
-    c.end = end;
-    c.b = lo;
-    c.tiles = tiles_of<E>(a, lo, &c.units);
-    const int64_t in = begin - shape.before[lo];
-    c.unit = (int)(in / c.tiles);
-    c.tile = (int)(in - (int64_t)c.unit * c.tiles);
+    const int tiles = tiles_of<E>(a, lo, a.pg.len[lo], &units);
+    const int unit = (int)((run_begin - before[lo]) / tiles);
+    place<E>(a, c, lo, unit, before[lo] + (int64_t)unit * tiles, run_begin, run_end);
   }
-  Cursor p = c;                                                           // the tile whose rows are copied next
-  Unit pu = unit_of<E>(a, p);
-  int p_unit = p.unit, p_b = p.b, page = 0;
-  uint32_t bad = 0;                                                       // stages whose page does not exist
+
+  // Copies run kStages - 1 tiles ahead of the products, into the next units where these end.
+  Part p = c;
   const uint32_t mine = smem_u32(stages) + warp * E::kStages * E::kStageBytes;
-  auto look_up = [&] {                                                    // the page of tile p (one tile ahead of its use)
-    if (p.pos >= p.end) return;
-    if (p.unit != p_unit || p.b != p_b) {
-      pu = unit_of<E>(a, p);
-      p_unit = p.unit;
-      p_b = p.b;
-    }
-    const int base = p.tile * E::kTile + warp * kWarpKeys;
-    if (base < pu.limit) page = __ldg(a.pg.table + pu.table + (base >> a.pg.page_shift));
+  const typename E::Lane ln(a, lane);
+  constexpr int kShift = E::kByteShift;                                   // bytes of a channel: 2^kShift (-1: half a byte)
+  auto bytes = [](int64_t channels) { return kShift < 0 ? channels >> 1 : channels << (kShift < 0 ? 0 : kShift); };
+  const int64_t page_bytes = bytes(a.pg.page_stride);
+  const uint32_t in_page = (1u << a.pg.page_shift) - 1u;
+  int left = 0, base_p = 0, page = 0;
+  int64_t head_bytes = 0;
+  const int32_t* table = nullptr;
+  uint32_t bad = 0;                                                       // stages whose page does not exist
+  bool more = true;
+  auto enter = [&] {
+    left = (int)(p.end - p.begin);
+    base_p = (int)(p.begin - p.unit_begin) * E::kTile + warp * kWarpKeys;
+    head_bytes = bytes(p.u.h * a.pg.head_stride);
+    table = a.pg.table + (int64_t)p.u.b * a.pg.table_stride;
+    if (base_p < p.u.limit) page = __ldg(table + (base_p >> a.pg.page_shift));
   };
   auto produce = [&](int slot) {
-    if (p.pos < p.end) {
-      const int base = p.tile * E::kTile + warp * kWarpKeys;
-      bad &= ~(1u << slot);
-      if (base < pu.limit) {
+    if (more) {
+      if (base_p < p.u.limit) {
+        bad &= ~(1u << slot);
         if ((unsigned)page < (unsigned)a.pg.n_pages) {
-          E::issue(a, mine + slot * E::kStageBytes,
-                   page * a.pg.page_stride + pu.h * a.pg.head_stride + (int64_t)(base & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride, lane);
+          E::issue(a, ln, mine + slot * E::kStageBytes, page * page_bytes + head_bytes + (int64_t)(base_p & in_page) * ln.rows, lane);
         } else {
           bad |= 1u << slot;
           if (lane == 0) atomicOr(a.status, kStatusBadPage);
         }
       }
-      advance<E>(a, p);
-      look_up();
+      base_p += E::kTile;
+      if (--left == 0) {
+        more = next<E>(a, p, before, run_end);
+        if (more) enter();
+      } else if (base_p < p.u.limit) {                                    // (looked up a tile before its use)
+        page = __ldg(table + (base_p >> a.pg.page_shift));
+      }
     }
     ptx::cp_async_commit();
   };
-  look_up();
+  enter();
   for (int st = 0; st < E::kStages - 1; ++st) produce(st);
 
   E e;
-  Unit u = unit_of<E>(a, c);
-  e.begin(a, u, extra, warp, lane);
-  int slot = 0;
-  for (; c.pos < c.end;) {
-    int ahead = slot + E::kStages - 1;
-    if (ahead >= E::kStages) ahead -= E::kStages;
-    produce(ahead);
-    ptx::cp_async_wait<E::kStages - 1>();
-    __syncwarp();
-    const int base = c.tile * E::kTile + warp * kWarpKeys;
-    if (base < u.limit && !((bad >> slot) & 1u)) e.step(a, u, mine + slot * E::kStageBytes, base, base + kWarpKeys <= u.full, extra, warp, lane);
-    __syncwarp();
-    if (++slot == E::kStages) slot = 0;
-    const int64_t unit_begin = c.pos - c.tile, unit_end = unit_begin + c.tiles;
-    if (c.tile + 1 < c.tiles && c.pos + 1 < c.end) {
-      advance<E>(a, c);
-      continue;
+  int slot = 0, ahead = E::kStages - 1;
+  for (bool on = true; on; on = next<E>(a, c, before, run_end)) {
+    e.begin(a, c.u, extra, warp, lane);
+    int base = (int)(c.begin - c.unit_begin) * E::kTile + warp * kWarpKeys;
+#pragma unroll 1
+    for (int n = (int)(c.end - c.begin); n > 0; --n, base += E::kTile) {
+      produce(ahead);
+      ptx::cp_async_wait<E::kStages - 1>();
+      __syncwarp();
+      if (base < c.u.limit && !((bad >> slot) & 1u)) {
+        if (base + kWarpKeys <= c.u.full) e.template step<true>(a, c.u, mine + slot * E::kStageBytes, base, extra, warp, lane);
+        else e.template step<false>(a, c.u, mine + slot * E::kStageBytes, base, extra, warp, lane);
+      }
+      __syncwarp();
+      ahead = slot;
+      slot = slot + 1 == E::kStages ? 0 : slot + 1;
     }
     // ---- the run leaves this unit
-    const bool alone = unit_begin >= begin && unit_end <= end;
-    const int64_t c0 = ((unit_begin + 1) * ctas - 1) / total, c1 = (unit_end * ctas - 1) / total;
-    constexpr int64_t kSlotFloats = (int64_t)kMaxRows * kPartRow;
-    float* const part = a.part + (2 * (int64_t)blockIdx.x + (unit_begin > begin ? 1 : 0)) * kSlotFloats;
+    const int64_t unit_end = c.unit_begin + c.tiles;
+    const bool alone = c.unit_begin >= run_begin && unit_end <= run_end;
+    const int64_t c0 = ((c.unit_begin + 1) * ctas - 1) / total, c1 = (unit_end * ctas - 1) / total;
+    float* const part = a.part + (2 * (int64_t)blockIdx.x + (c.unit_begin > run_begin ? 1 : 0)) * kSlotFloats;
     for (int nt = 0; nt < E::kNT; ++nt) {
       __syncthreads();
       e.flush(buf + warp * kBufRow, ml + warp * 8, nt, lane);
@@ -711,12 +792,10 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
           acc = make_float4(fmaf(f, x.x, acc.x), fmaf(f, x.y, acc.y), fmaf(f, x.z, acc.z), fmaf(f, x.w, acc.w));
         }
         if (alone) {
-          write_row<E>(a, u, 8 * nt + r, acc, top, sum, lane);
+          write_row<E>(a, c.u, 8 * nt + r, acc, top, sum, lane);
         } else {
-          float* to = part + (8 * nt + r) * kPartRow;
-          __stcg(reinterpret_cast<float2*>(to + 4 * lane), make_float2(acc.x, acc.y));
-          __stcg(reinterpret_cast<float2*>(to + 4 * lane + 2), make_float2(acc.z, acc.w));
-          if (lane == 0) __stcg(reinterpret_cast<float2*>(to + kHeadDim), make_float2(top, sum));
+          __stcg(reinterpret_cast<float4*>(part + (8 * nt + r) * kHeadDim) + lane, acc);
+          if (lane == 0) __stcg(reinterpret_cast<float2*>(part + kMaxRows * kHeadDim) + 8 * nt + r, make_float2(top, sum));
         }
       }
     }
@@ -727,37 +806,14 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
       __syncthreads();
       if (last_here) {
         __threadfence();
-        const bool inside = unit_begin > total * c0 / ctas;               // (the first CTA's part: behind another one of its own)
+        const bool inside = c.unit_begin > total * c0 / ctas;             // (the first CTA's part: behind another one of its own)
         const float* first = a.part + (2 * c0 + (inside ? 1 : 0)) * kSlotFloats;
         const int n = (int)(c1 - c0) + 1;
-        for (int r = warp; r < E::kRows; r += E::kWarps) {
-          auto from = [&](int x) { return (x == 0 ? first : a.part + 2 * (c0 + x) * kSlotFloats) + r * kPartRow; };
-          float top = kLowest;
-          for (int x = lane; x < n; x += 32) top = fmaxf(top, __ldcg(from(x) + kHeadDim));
-#pragma unroll
-          for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          float sum = 0.f;
-#pragma unroll 8
-          for (int x = 0; x < n; ++x) {
-            const float* at = from(x);
-            const float2 mx = __ldcg(reinterpret_cast<const float2*>(at + kHeadDim)), lo = __ldcg(reinterpret_cast<const float2*>(at + 4 * lane)),
-                         hi = __ldcg(reinterpret_cast<const float2*>(at + 4 * lane + 2));
-            const float f = ex2(mx.x - top);
-            sum = fmaf(f, mx.y, sum);
-            acc = make_float4(fmaf(f, lo.x, acc.x), fmaf(f, lo.y, acc.y), fmaf(f, hi.x, acc.z), fmaf(f, hi.y, acc.w));
-          }
-          write_row<E>(a, u, r, acc, top, sum, lane);
-        }
+        for (int r = warp; r < E::kRows; r += E::kWarps) merge_row<E>(a, c.u, r, first, a.part + 2 * c0 * kSlotFloats, n, lane);
         if (threadIdx.x == 0) a.sync[c0] = 0u;
       }
     }
-    advance<E>(a, c);
-    if (c.pos < c.end) {
-      u = unit_of<E>(a, c);
-      __syncthreads();
-      e.begin(a, u, extra, warp, lane);
-    }
+    __syncthreads();
   }
   ptx::cp_async_wait<0>();
 }
@@ -777,7 +833,7 @@ cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
 
 }  // namespace
 
-size_t attend_part_floats(int n_sm) { return (size_t)2 * n_sm * kMaxCtasPerSm * kMaxRows * kPartRow; }
+size_t attend_part_floats(int n_sm) { return (size_t)2 * n_sm * kMaxCtasPerSm * kSlotFloats; }
 size_t attend_sync_words(int n_sm) { return (size_t)n_sm * kMaxCtasPerSm; }
 
 cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t, const Dims& dm, const void* q, int64_t q_stride, float softcap, void* out,

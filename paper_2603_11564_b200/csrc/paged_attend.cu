@@ -24,10 +24,9 @@ namespace {
 using ptx::ex2;
 using ptx::smem_u32;
 
-constexpr int kWarpKeys = 16;
 constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
 constexpr int kPadRow = 132;                         // floats of a row of the warps' partial outputs (conflict-free, see flush)
-constexpr int kMaxRows = 16, kMaxCtasPerSm = 2;
+constexpr int kMaxRows = 16, kMaxCtasPerSm = 2, kMostSms = 160;   // (more SMs than that: one wave on 160 of them)
 constexpr int kSlotFloats = kMaxRows * (kHeadDim + 2);   // a partial result: [rows][128] outputs, [rows] maxima and sums
 
 struct Attend {
@@ -168,8 +167,8 @@ __device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
 template <bool kFp4, int kTiles>
 struct TensorEngine {
   static constexpr int kNT = kTiles;
-  static constexpr int kWarps = kFp4 && kNT == 1 ? 16 : 8, kTile = kWarps * kWarpKeys, kRows = 8 * kNT, kCtas = 1, kStages = kFp4 ? 4 : 3, kMinRun = 4, kByteShift = kFp4 ? -1 : 1;
-  static constexpr int kStageBytes = kFp4 ? kWarpKeys * 144 : kWarpKeys * 512;
+  static constexpr int kWarps = 8, kSub = kFp4 && kNT == 1 ? 2 : 1, kTile = kWarps * kSub * 16, kRows = 8 * kNT, kCtas = 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kMinRun = 2, kByteShift = kFp4 ? -1 : 1, kSubBytes = kFp4 ? 16 * 144 : 16 * 512, kStageBytes = kSub * kSubBytes;
   static constexpr int kExtra = 0;
   static constexpr float kLift = kFp4 ? 11.f : 0.f;
   using T = __nv_bfloat16;
@@ -266,17 +265,15 @@ struct TensorEngine {
     }
   }
 
-  // Keys base .. base + 15 of the sequence; whole: all of the unit's queries see all of them.
-  template <bool whole>
-  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char*, int, int lane) {
+  // The logits of 16 keys: rows key_of(g) and key_of(g) + 8, query rows 2 t and 2 t + 1 of every eight.
+  __device__ __forceinline__ void logits(uint32_t stage, int lane, float (&s)[kNT][4]) const {
     const int g = lane >> 2, t = lane & 3, rk = key_of(g);
-    float s[kNT][4];
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
     if (kFp4) {
-      const uint4 ka = ptx::lds128(stage + piece4(rk, t)), kb = ptx::lds128(stage + piece4(rk + 8, t));
+      const uint4 ka = ptx::lds128(stage + piece4(rk, t)), kb = ptx::lds128(stage + piece4(rk, t) + 512);
       const uint32_t sa = scales_to_half(lds_u16(stage + 2048 + 8 * rk + 2 * t)), sb = scales_to_half(lds_u16(stage + 2048 + 8 * rk + 64 + 2 * t));
       const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
 #pragma unroll
@@ -305,69 +302,21 @@ struct TensorEngine {
         }
       }
     }
-    // base-2 logits
-    float z[kNT][4];
-    bool above = false;
-#pragma unroll
-    for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        z[nt][e] = s[nt][e] * fac[nt][e & 1];
-        if (a.softcap > 0.f) z[nt][e] = capped(z[nt][e], a.softcap * 1.44269504f);
-        if (!whole && base + rk + (e & 2) * 4 >= lim[nt][e & 1]) z[nt][e] = -CUDART_INF_F;
-        above = above || z[nt][e] > m[nt][e & 1] + kSlack;
-      }
-    if (__any_sync(0xffffffffu, above)) {
-#pragma unroll
-      for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float top = fmaxf(z[nt][e], z[nt][e + 2]);
-#pragma unroll
-          for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-          top = fmaxf(top, m[nt][e]);
-          const float f = ex2(m[nt][e] - top);
-          m[nt][e] = top;
-          l[nt][e] *= f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            o[nt][j][e] *= f;
-            o[nt][j][e + 2] *= f;
-          }
-        }
-    }
-    uint32_t p0[kNT], p1[kNT];
-#pragma unroll
-    for (int nt = 0; nt < kNT; ++nt) {
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[e] = ex2(z[nt][e] - m[nt][e & 1] + kLift);
-        l[nt][e & 1] += p[e];
-      }
-      uint32_t lo, hi;
-      if (kFp4) {
-        lo = bits(__floats2half2_rn(p[0], p[1]));
-        hi = bits(__floats2half2_rn(p[2], p[3]));
-      } else {
-        const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
-        lo = *reinterpret_cast<const uint32_t*>(&x);
-        hi = *reinterpret_cast<const uint32_t*>(&y);
-      }
-      p0[nt] = transpose8x8(lo);
-      p1[nt] = transpose8x8(hi);
-    }
-    // indices 2t, 2t + 1, 2t + 8, 2t + 9 of the contraction; rows behind the last visible one may hold anything
-    const int rv[4] = {t, 4 + (t ^ 1), 8 + t, 12 + (t ^ 1)};
+  }
+  // The outputs of 16 keys with weights p0, p1 (indices 2 t, 2 t + 1 and 2 t + 8, 2 t + 9 of the contraction for row g).
+  template <bool whole>
+  __device__ __forceinline__ void outputs(uint32_t stage, int lane, int base, int limit, const uint32_t (&p0)[kNT], const uint32_t (&p1)[kNT]) {
+    const int g = lane >> 2, t = lane & 3;
+    const int rv[4] = {t, 4 + (t ^ 1), 8 + t, 12 + (t ^ 1)};               // rows behind the last visible one may hold anything
     if (kFp4) {
       uint32_t w[4][2], sc[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint2 x = lds64(stage + 1024 + piece4(rv[i], g >> 1) + 8 * (g & 1));
+        const uint2 x = lds64(stage + 1024 + piece4(rv[i & 1], g >> 1) + 8 * (g & 1) + 512 * (i >> 1));
         w[i][0] = x.x;
         w[i][1] = x.y;
-        sc[i] = lds_u8(stage + 2176 + 8 * rv[i] + g);
-        if (!whole && base + rv[i] >= u.limit) sc[i] = 0;
+        sc[i] = lds_u8(stage + 2176 + 8 * rv[i & 1] + g + 64 * (i >> 1));
+        if (!whole && base + rv[i] >= limit) sc[i] = 0;
       }
       const __half2 f01 = halves(scales_to_half(sc[0] | (sc[1] << 8))), f23 = halves(scales_to_half(sc[2] | (sc[3] << 8)));
 #pragma unroll
@@ -390,7 +339,7 @@ struct TensorEngine {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           w[i] = ptx::lds128(stage + 4096 + piece16(rv[i], g + 8 * hf));
-          if (!whole && base + rv[i] >= u.limit) w[i] = make_uint4(0, 0, 0, 0);
+          if (!whole && base + rv[i] >= limit) w[i] = make_uint4(0, 0, 0, 0);
         }
         const uint32_t* x[4] = {&w[0].x, &w[1].x, &w[2].x, &w[3].x};
 #pragma unroll
@@ -401,6 +350,73 @@ struct TensorEngine {
           for (int nt = 0; nt < kNT; ++nt) mma<false>(o[nt][4 * hf + j], a0, a1, a2, a3, p0[nt], p1[nt]);
         }
       }
+    }
+  }
+  // Keys base .. base + 16 kSub - 1 of the sequence; whole: all of the unit's queries see all of them; gone: pieces of 16 that do not exist.
+  template <bool whole>
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char*, int, int lane, uint32_t gone = 0u) {
+    const int rk = key_of(lane >> 2);
+    float z[kSub][kNT][4];                                                 // base-2 logits
+    bool above = false;
+#pragma unroll
+    for (int b = 0; b < kSub; ++b) logits(stage + b * kSubBytes, lane, z[b]);
+#pragma unroll
+    for (int b = 0; b < kSub; ++b)
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float& x = z[b][nt][e];
+          x *= fac[nt][e & 1];
+          if (a.softcap > 0.f) x = capped(x, a.softcap * 1.44269504f);
+          if (!whole && (base + 16 * b + rk + (e & 2) * 4 >= lim[nt][e & 1] || ((gone >> b) & 1u))) x = -CUDART_INF_F;
+          above = above || x > m[nt][e & 1] + kSlack;
+        }
+    if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = fmaxf(z[0][nt][e], z[0][nt][e + 2]);
+#pragma unroll
+          for (int b = 1; b < kSub; ++b) top = fmaxf(top, fmaxf(z[b][nt][e], z[b][nt][e + 2]));
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+          top = fmaxf(top, m[nt][e]);
+          const float f = ex2(m[nt][e] - top);
+          m[nt][e] = top;
+          l[nt][e] *= f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            o[nt][j][e] *= f;
+            o[nt][j][e + 2] *= f;
+          }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < kSub; ++b) {
+      uint32_t p0[kNT], p1[kNT];
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = ex2(z[b][nt][e] - (m[nt][e & 1] - kLift));
+          l[nt][e & 1] += p[e];
+        }
+        uint32_t lo, hi;
+        if (kFp4) {
+          lo = bits(__floats2half2_rn(p[0], p[1]));
+          hi = bits(__floats2half2_rn(p[2], p[3]));
+        } else {
+          const __nv_bfloat162 x = __floats2bfloat162_rn(p[0], p[1]), y = __floats2bfloat162_rn(p[2], p[3]);
+          lo = *reinterpret_cast<const uint32_t*>(&x);
+          hi = *reinterpret_cast<const uint32_t*>(&y);
+        }
+        p0[nt] = transpose8x8(lo);
+        p1[nt] = transpose8x8(hi);
+      }
+      outputs<whole>(stage + b * kSubBytes, lane, base + 16 * b, !whole && ((gone >> b) & 1u) ? 0 : u.limit, p0, p1);
     }
   }
 
@@ -433,9 +449,9 @@ struct TensorEngine {
 // outputs, queries and weights broadcast from shared memory.
 template <bool kFp4>
 struct FloatEngine {
-  static constexpr int kWarps = 4, kTile = kWarps * kWarpKeys, kRows = 8, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
-  static constexpr int kStageBytes = kFp4 ? kWarpKeys * 144 : kWarpKeys * 1024;
-  static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = kWarpKeys * kRows * 4;
+  static constexpr int kWarps = 4, kSub = 1, kTile = kWarps * 16, kRows = 8, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
+  static constexpr int kSubBytes = kFp4 ? 16 * 144 : 16 * 1024, kStageBytes = kSubBytes;
+  static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = 16 * kRows * 4;
   static constexpr int kExtra = kQBytes + kWarps * kPBytes;
   static constexpr float kLift = 0.f;
   static constexpr int kNT = 1;
@@ -460,7 +476,7 @@ struct FloatEngine {
     } else {
       const char *k = a.pg.k + off + ln.from, *v = a.pg.v + off + ln.from;
 #pragma unroll
-      for (int r = 0; r < kWarpKeys; ++r) {
+      for (int r = 0; r < 16; ++r) {
         ptx::cp_async16(stage + piece32(r, lane), k + r * ln.rows);
         ptx::cp_async16(stage + 8192 + piece32(r, lane), v + r * ln.rows);
       }
@@ -487,7 +503,8 @@ struct FloatEngine {
   }
 
   template <bool whole>
-  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char* extra, int warp, int lane) {
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char* extra, int warp, int lane, uint32_t gone = 0u) {
+    if (!whole && gone) return;
     const int key = lane >> 1, hf = lane & 1;
     const uint32_t qs = smem_u32(extra), ps = qs + kQBytes + warp * kPBytes;
     float s[kRows];
@@ -559,7 +576,7 @@ struct FloatEngine {
       asm volatile("st.shared.f32 [%0], %1;" ::"r"(ps + (key * kRows + 2 * i + hf) * 4), "f"(p) : "memory");
     }
     __syncwarp();
-    const int keys = min(kWarpKeys, u.limit - base);                      // rows behind the last visible one may hold anything
+    const int keys = min(16, u.limit - base);                      // rows behind the last visible one may hold anything
     for (int k = 0; k < keys; ++k) {
       float4 v;
       if (kFp4) {
@@ -616,34 +633,46 @@ __device__ __forceinline__ void write_row(const Attend& a, const Unit& u, int r,
   if (a.lse != nullptr && lane == 0) a.lse[at] = sum == 0.f ? -CUDART_INF_F : (top - E::kLift + log2f(sum)) * 0.69314718f;
 }
 
-// Row r of a unit from the partial results of n CTAs, in their order: the first one's at `first`, the x-th one's at others + 2 x slots.  A
-// warp's loads of kBatch of them are in flight together (one after the other they cost 25 us for the 74 of a cache of 128k rows).
+// Row r of a unit from the partial results of n CTAs, in their order: the first one's at `first`, the x-th one's at others + 2 x slots.  What a
+// warp waits for is latency, so its loads are in flight together: all maxima and sums, and kBatch outputs at a time.
 template <class E>
 __device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r, const float* first, const float* others, int n, int lane) {
-  constexpr int kBatch = 8;
+  constexpr int kBatch = 16, kStats = kMostSms * E::kCtas / 32;
   auto from = [&](int x) { return x == 0 ? first : others + 2 * (int64_t)x * kSlotFloats; };
-  auto stats = [&](int x) { return __ldcg(reinterpret_cast<const float2*>(from(x) + kMaxRows * kHeadDim) + r); };
-  float top = kLowest;
-  for (int x = lane; x < n; x += 32) top = fmaxf(top, stats(x).x);
+  float4 v[kBatch];
+  auto load = [&](int x0) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(from(min(x0 + i, n - 1)) + r * kHeadDim) + lane);
+  };
+  float weight[kStats], sum = 0.f, top = kLowest;
+  float2 st[kStats];
+#pragma unroll
+  for (int i = 0; i < kStats; ++i) {
+    st[i] = make_float2(kLowest, 0.f);
+    if (32 * i + lane < n) st[i] = __ldcg(reinterpret_cast<const float2*>(from(32 * i + lane) + kMaxRows * kHeadDim) + r);
+  }
+  load(0);
+#pragma unroll
+  for (int i = 0; i < kStats; ++i) top = fmaxf(top, st[i].x);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+#pragma unroll
+  for (int i = 0; i < kStats; ++i) {
+    weight[i] = 32 * i + lane < n ? ex2(st[i].x - top) : 0.f;
+    sum = fmaf(weight[i], st[i].y, sum);
+  }
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float sum = 0.f;
-  for (int x0 = 0; x0 < n; x0 += 32) {
-    float weight = 0.f;
-    if (x0 + lane < n) {
-      const float2 mx = stats(x0 + lane);
-      weight = ex2(mx.x - top);
-      sum = fmaf(weight, mx.y, sum);
-    }
-    for (int x1 = x0; x1 < min(x0 + 32, n); x1 += kBatch) {
-      float4 v[kBatch];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(from(min(x1 + i, n - 1)) + r * kHeadDim) + lane);
+  for (int i = 0; i < kStats; ++i) {
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const float f = __shfl_sync(0xffffffffu, weight, x1 - x0 + i);    // (0 behind the last one)
-        if (x1 + i < n) acc = make_float4(fmaf(f, v[i].x, acc.x), fmaf(f, v[i].y, acc.y), fmaf(f, v[i].z, acc.z), fmaf(f, v[i].w, acc.w));
+    for (int h = 0; h < 32; h += kBatch) {
+      const int x0 = 32 * i + h;
+      if (x0 >= n) break;
+      if (x0 > 0) load(x0);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const float f = __shfl_sync(0xffffffffu, weight[i], h + k);
+        if (x0 + k < n) acc = make_float4(fmaf(f, v[k].x, acc.x), fmaf(f, v[k].y, acc.y), fmaf(f, v[k].z, acc.z), fmaf(f, v[k].w, acc.w));
       }
     }
   }
@@ -716,35 +745,44 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
   auto bytes = [](int64_t channels) { return kShift < 0 ? channels >> 1 : channels << (kShift < 0 ? 0 : kShift); };
   const int64_t page_bytes = bytes(a.pg.page_stride);
   const uint32_t in_page = (1u << a.pg.page_shift) - 1u;
-  int left = 0, base_p = 0, page = 0;
+  int left = 0, base_p = 0, page[E::kSub] = {};
   int64_t head_bytes = 0;
   const int32_t* table = nullptr;
-  uint32_t bad = 0;                                                       // stages whose page does not exist
+  uint32_t bad = 0;                                                       // pieces of stages whose page does not exist
   bool more = true;
+  auto look_up = [&] {                                                    // (a tile before its use)
+#pragma unroll
+    for (int b = 0; b < E::kSub; ++b)
+      if (base_p + 16 * b < p.u.limit) page[b] = __ldg(table + ((base_p + 16 * b) >> a.pg.page_shift));
+  };
   auto enter = [&] {
     left = (int)(p.end - p.begin);
-    base_p = (int)(p.begin - p.unit_begin) * E::kTile + warp * kWarpKeys;
+    base_p = (int)(p.begin - p.unit_begin) * E::kTile + warp * (16 * E::kSub);
     head_bytes = bytes(p.u.h * a.pg.head_stride);
     table = a.pg.table + (int64_t)p.u.b * a.pg.table_stride;
-    if (base_p < p.u.limit) page = __ldg(table + (base_p >> a.pg.page_shift));
+    look_up();
   };
   auto produce = [&](int slot) {
     if (more) {
-      if (base_p < p.u.limit) {
-        bad &= ~(1u << slot);
-        if ((unsigned)page < (unsigned)a.pg.n_pages) {
-          E::issue(a, ln, mine + slot * E::kStageBytes, page * page_bytes + head_bytes + (int64_t)(base_p & in_page) * ln.rows, lane);
-        } else {
-          bad |= 1u << slot;
-          if (lane == 0) atomicOr(a.status, kStatusBadPage);
+      bad &= ~(((1u << E::kSub) - 1u) << (slot * E::kSub));
+#pragma unroll
+      for (int b = 0; b < E::kSub; ++b) {
+        const int row = base_p + 16 * b;
+        if (row < p.u.limit) {
+          if ((unsigned)page[b] < (unsigned)a.pg.n_pages) {
+            E::issue(a, ln, mine + slot * E::kStageBytes + b * E::kSubBytes, page[b] * page_bytes + head_bytes + (int64_t)(row & in_page) * ln.rows, lane);
+          } else {
+            bad |= 1u << (slot * E::kSub + b);
+            if (lane == 0) atomicOr(a.status, kStatusBadPage);
+          }
         }
       }
       base_p += E::kTile;
       if (--left == 0) {
         more = next<E>(a, p, before, run_end);
         if (more) enter();
-      } else if (base_p < p.u.limit) {                                    // (looked up a tile before its use)
-        page = __ldg(table + (base_p >> a.pg.page_shift));
+      } else {
+        look_up();
       }
     }
     ptx::cp_async_commit();
@@ -756,15 +794,17 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
   int slot = 0, ahead = E::kStages - 1;
   for (bool on = true; on; on = next<E>(a, c, before, run_end)) {
     e.begin(a, c.u, extra, warp, lane);
-    int base = (int)(c.begin - c.unit_begin) * E::kTile + warp * kWarpKeys;
+    int base = (int)(c.begin - c.unit_begin) * E::kTile + warp * (16 * E::kSub);
 #pragma unroll 1
     for (int n = (int)(c.end - c.begin); n > 0; --n, base += E::kTile) {
       produce(ahead);
       ptx::cp_async_wait<E::kStages - 1>();
       __syncwarp();
-      if (base < c.u.limit && !((bad >> slot) & 1u)) {
-        if (base + kWarpKeys <= c.u.full) e.template step<true>(a, c.u, mine + slot * E::kStageBytes, base, extra, warp, lane);
-        else e.template step<false>(a, c.u, mine + slot * E::kStageBytes, base, extra, warp, lane);
+      const uint32_t stage = mine + slot * E::kStageBytes, gone = (bad >> (slot * E::kSub)) & ((1u << E::kSub) - 1u);
+      if (base + 16 * E::kSub <= c.u.full && gone == 0u) {
+        e.template step<true>(a, c.u, stage, base, extra, warp, lane);
+      } else if (base < c.u.limit) {
+        e.template step<false>(a, c.u, stage, base, extra, warp, lane, gone);
       }
       __syncwarp();
       ahead = slot;
@@ -827,14 +867,14 @@ cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
   int64_t most = 0;
   const int64_t tiles = (((int64_t)a.pg.table_stride << a.pg.page_shift) + E::kTile - 1) / E::kTile;
   for (int b = 0; b < a.t.batch; ++b) most += (int64_t)a.n_kv_heads * (((int64_t)(a.t.cu[b + 1] - a.t.cu[b]) * a.group + E::kRows - 1) / E::kRows) * tiles;
-  const int64_t grid = (int64_t)n_sm * E::kCtas;
+  const int64_t grid = (int64_t)min(n_sm, kMostSms) * E::kCtas;
   return launch_pdl(paged_attend_kernel<E>, dim3((unsigned)(most < grid ? most : grid)), dim3(E::kWarps * 32), smem, s, 1, a);
 }
 
 }  // namespace
 
-size_t attend_part_floats(int n_sm) { return (size_t)2 * n_sm * kMaxCtasPerSm * kSlotFloats; }
-size_t attend_sync_words(int n_sm) { return (size_t)n_sm * kMaxCtasPerSm; }
+size_t attend_part_floats(int n_sm) { return (size_t)2 * min(n_sm, kMostSms) * kMaxCtasPerSm * kSlotFloats; }
+size_t attend_sync_words(int n_sm) { return (size_t)min(n_sm, kMostSms) * kMaxCtasPerSm; }
 
 cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t, const Dims& dm, const void* q, int64_t q_stride, float softcap, void* out,
                                 float* lse, float* part, uint32_t* sync, int n_sm, int* status, cudaStream_t s, LaunchLog* log) {

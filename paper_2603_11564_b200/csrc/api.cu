@@ -428,7 +428,7 @@ dapq_status dapq_create(dapq_ctx** out, const dapq_shape* sh, int device) {
     if (n_slots > 1) ar.add(&ctx->slots, nl * n_slots * score_bytes);
     if (flow)
       for (auto& w : ctx->sync) ar.add(&w, ctx->sync_words * sizeof(uint32_t));
-    ar.add(&ctx->attend_part, attend_part_floats(ctx->n_sm) * sizeof(float));
+    ar.add(&ctx->attend_part, attend_part_floats(ctx->n_sm, sh->dtype == DAPQ_BF16) * sizeof(float));
     ar.add(&ctx->attend_sync, attend_sync_words(ctx->n_sm) * sizeof(uint32_t));
     return ar.allocate(ctx);
   };
@@ -1215,7 +1215,7 @@ dapq_status dapq_paged_attend(dapq_ctx* ctx, const dapq_paged_cache* pages, cons
   if (t.cu[t.batch] == 0) return DAPQ_OK;
   DeviceGuard guard(ctx->device);
   cudaError_t e = launch_paged_attend(ctx->shape.dtype, pg, t, ctx->dims, q, q_token_stride, softcap, out, lse_out, ctx->attend_part, ctx->attend_sync, ctx->n_sm,
-                                      ctx->status, (cudaStream_t)stream, &ctx->log);
+                                      ctx->status, ctx->wait_limit, (cudaStream_t)stream, &ctx->log);
   if (e != cudaSuccess) return cuda_fail(ctx, e, "paged attention kernel");
   return DAPQ_OK;
 }

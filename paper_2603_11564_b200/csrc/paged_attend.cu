@@ -15,32 +15,12 @@
 //
 // Softmax: base 2, against a maximum that is only moved when a logit exceeds it by more than kSlack, so that most tiles need neither
 // a reduction nor a rescaling.
-#include "paged.cuh"
-#include "umma_ptx.cuh"
+#include "paged_attend.cuh"
 
 namespace dapq {
 namespace {
 
-using ptx::ex2;
-using ptx::smem_u32;
-
-constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
 constexpr int kPadRow = 132;                         // floats of a row of the warps' partial outputs (conflict-free, see flush)
-constexpr int kMaxRows = 16, kMaxCtasPerSm = 2, kMostSms = 160;   // (more SMs than that: one wave on 160 of them)
-constexpr int kSlotFloats = kMaxRows * (kHeadDim + 2);   // a partial result: [rows][128] outputs, [rows] maxima and sums
-
-struct Attend {
-  PagedDev pg;
-  NewRows t;
-  const void* q;
-  int64_t q_stride;
-  void* out;
-  float *lse, *part;
-  uint32_t* sync;
-  int* status;
-  int32_t n_q_heads, n_kv_heads, group;
-  float scale_log2e, softcap;
-};
 
 // ---- pieces ---------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
@@ -87,76 +67,6 @@ __device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// c tanh(x / c) log2(e) of x = y c / (2 log2(e)), through the exponential (the tanh instruction has 11 bits).
-__device__ __forceinline__ float capped(float y, float c_log2e) { return c_log2e - __fdividef(2.f * c_log2e, 1.f + ex2(y)); }
-
-// What a unit is: a row tile of one sequence and KV head.
-struct Unit {
-  int b, h, row0;          // first query row; row r is query r / group of the sequence, head h * group + r % group
-  int rows;                // rows of the sequence
-  int held, limit;         // rows held before the step, end of the rows that any of the tile's queries sees
-  int full;                // end of the rows that all of them see
-};
-
-// Tiles of a sequence's units, and their number.
-template <class E>
-__device__ __forceinline__ int tiles_of(const Attend& a, int b, int held, int* units) {
-  const int n = a.t.cu[b + 1] - a.t.cu[b];
-  *units = a.n_kv_heads * ((n * a.group + E::kRows - 1) / E::kRows);
-  const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift, rows = held < 0 ? 0 : min((int64_t)held + n, room);
-  return n == 0 ? 0 : max(1, (int)((rows + E::kTile - 1) / E::kTile));
-}
-
-// A part of a CTA's run of tiles that lies in one unit.
-struct Part {
-  int64_t begin, end, unit_begin;                    // tiles of the call: [begin, end) of the unit's [unit_begin, unit_begin + tiles)
-  int tiles, unit;                                   // of the sequence u.b
-  Unit u;
-};
-
-template <class E>
-__device__ __forceinline__ void place(const Attend& a, Part& p, int b, int unit, int64_t unit_begin, int64_t begin, int64_t run_end) {
-  const int n = a.t.cu[b + 1] - a.t.cu[b], held = a.pg.len[b];
-  int units;
-  p.tiles = tiles_of<E>(a, b, held, &units);
-  p.unit = unit;
-  p.unit_begin = unit_begin;
-  p.begin = begin;
-  p.end = min(run_end, unit_begin + p.tiles);
-  Unit& u = p.u;
-  u.b = b;
-  u.rows = n * a.group;
-  const int row_tiles = units / a.n_kv_heads;
-  u.h = unit / row_tiles;
-  u.row0 = (unit - u.h * row_tiles) * E::kRows;
-  u.held = held;
-  const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift;
-  const int first = u.row0 / a.group, last = min((u.row0 + E::kRows - 1) / a.group, n - 1);
-  u.limit = held < 0 ? 0 : (int)min((int64_t)held + last + 1, room);
-  u.full = held < 0 ? 0 : (int)min((int64_t)held + first + 1, room);
-}
-// The part of the run behind p, if there is one.
-template <class E>
-__device__ __forceinline__ bool next(const Attend& a, Part& p, const int64_t* before, int64_t run_end) {
-  if (p.end >= run_end) {
-    p.begin = p.end;
-    return false;
-  }
-  const int64_t at = p.end;                          // (the part ended with its unit)
-  int b = p.u.b, unit = p.unit + 1;
-  if (at >= before[b + 1]) {
-    unit = 0;
-    do ++b; while (before[b + 1] <= at);
-  }
-  place<E>(a, p, b, unit, at, at, run_end);
-  return true;
-}
-// Rows that query row r of the unit sees.
-__device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
-  const int row = u.row0 + r;
-  return row < u.rows && u.held >= 0 ? (int)min((int64_t)u.held + row / a.group + 1, (int64_t)u.limit) : 0;
-}
-
 // ---- 16 keys of a warp on the tensor cores ----------------------------------------------------------------------------
 // Products: S^T = K Q^T, m16n8k16 with the 16 keys as rows; O^T += V^T P^T with 16 channels as rows and the keys as k.  Which key is row r of the
 // one and index r of the other is free as long as it is the same, and so is which channel is which index of the contraction:
@@ -167,7 +77,7 @@ __device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
 template <bool kFp4, int kTiles>
 struct TensorEngine {
   static constexpr int kNT = kTiles;
-  static constexpr int kWarps = 8, kSub = kFp4 && kNT == 1 ? 2 : 1, kTile = kWarps * kSub * 16, kRows = 8 * kNT, kCtas = 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kWarps = 8, kSub = kFp4 && kNT == 1 ? 2 : 1, kTile = kWarps * kSub * 16, kRows = 8 * kNT, kSlotRows = 16, kCtas = 1, kStages = kFp4 ? 4 : 3;
   static constexpr int kMinRun = 2, kByteShift = kFp4 ? -1 : 1, kSubBytes = kFp4 ? 16 * 144 : 16 * 512, kStageBytes = kSub * kSubBytes;
   static constexpr int kExtra = 0;
   static constexpr float kLift = kFp4 ? 11.f : 0.f;
@@ -228,7 +138,7 @@ struct TensorEngine {
       uint4 w[4] = {};
       if (row < u.rows) {
         const int i = row / a.group, h = u.h * a.group + row - i * a.group;
-        const uint4* src = reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(a.t.cu[u.b] + i) * a.q_stride + h * kHeadDim);
+        const uint4* src = reinterpret_cast<const uint4*>((const T*)a.q + (int64_t)(a.start[u.b] + i) * a.q_stride + h * kHeadDim);
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = __ldg(src + (kFp4 ? 4 * t + j : 2 * t + (j & 1) + 8 * (j >> 1)));
       }
@@ -449,7 +359,7 @@ struct TensorEngine {
 // outputs, queries and weights broadcast from shared memory.
 template <bool kFp4>
 struct FloatEngine {
-  static constexpr int kWarps = 4, kSub = 1, kTile = kWarps * 16, kRows = 8, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
+  static constexpr int kWarps = 4, kSub = 1, kTile = kWarps * 16, kRows = 8, kSlotRows = 16, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
   static constexpr int kSubBytes = kFp4 ? 16 * 144 : 16 * 1024, kStageBytes = kSubBytes;
   static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = 16 * kRows * 4;
   static constexpr int kExtra = kQBytes + kWarps * kPBytes;
@@ -487,7 +397,7 @@ struct FloatEngine {
     for (int x = threadIdx.x; x < kRows * kHeadDim / 4; x += kWarps * 32) {
       const int row = u.row0 + x / (kHeadDim / 4), i = row / a.group, h = u.h * a.group + row - i * a.group;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (row < u.rows) v = __ldg(reinterpret_cast<const float4*>((const T*)a.q + (int64_t)(a.t.cu[u.b] + i) * a.q_stride + h * kHeadDim) + x % (kHeadDim / 4));
+      if (row < u.rows) v = __ldg(reinterpret_cast<const float4*>((const T*)a.q + (int64_t)(a.start[u.b] + i) * a.q_stride + h * kHeadDim) + x % (kHeadDim / 4));
       reinterpret_cast<float4*>(extra)[x] = v;
     }
     __syncthreads();
@@ -616,71 +526,6 @@ struct FloatEngine {
 };
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void store2(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
-__device__ __forceinline__ void store2(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
-
-// Positions 4 lane .. 4 lane + 3 of row r of the unit, weights summing to `sum` against the maximum `top`.
-template <class E>
-__device__ __forceinline__ void write_row(const Attend& a, const Unit& u, int r, float4 acc, float top, float sum, int lane) {
-  const int row = u.row0 + r;
-  if (row >= u.rows) return;
-  const int i = row / a.group, h = u.h * a.group + row - i * a.group;
-  const int64_t at = (int64_t)(a.t.cu[u.b] + i) * a.n_q_heads + h;
-  const float f = sum == 0.f ? 0.f : (a.pg.fp4 ? a.pg.v_scale : 1.f) / sum;
-  typename E::T* out = (typename E::T*)a.out + at * kHeadDim;
-  store2(out + E::channel(4 * lane), acc.x * f, acc.y * f);
-  store2(out + E::channel(4 * lane + 2), acc.z * f, acc.w * f);
-  if (a.lse != nullptr && lane == 0) a.lse[at] = sum == 0.f ? -CUDART_INF_F : (top - E::kLift + log2f(sum)) * 0.69314718f;
-}
-
-// Row r of a unit from the partial results of n CTAs, in their order: the first one's at `first`, the x-th one's at others + 2 x slots.  What a
-// warp waits for is latency, so its loads are in flight together: all maxima and sums, and kBatch outputs at a time.
-template <class E>
-__device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r, const float* first, const float* others, int n, int lane) {
-  constexpr int kBatch = 16, kStats = kMostSms * E::kCtas / 32;
-  auto from = [&](int x) { return x == 0 ? first : others + 2 * (int64_t)x * kSlotFloats; };
-  float4 v[kBatch];
-  auto load = [&](int x0) {
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(from(min(x0 + i, n - 1)) + r * kHeadDim) + lane);
-  };
-  float weight[kStats], sum = 0.f, top = kLowest;
-  float2 st[kStats];
-#pragma unroll
-  for (int i = 0; i < kStats; ++i) {
-    st[i] = make_float2(kLowest, 0.f);
-    if (32 * i + lane < n) st[i] = __ldcg(reinterpret_cast<const float2*>(from(32 * i + lane) + kMaxRows * kHeadDim) + r);
-  }
-  load(0);
-#pragma unroll
-  for (int i = 0; i < kStats; ++i) top = fmaxf(top, st[i].x);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-#pragma unroll
-  for (int i = 0; i < kStats; ++i) {
-    weight[i] = 32 * i + lane < n ? ex2(st[i].x - top) : 0.f;
-    sum = fmaf(weight[i], st[i].y, sum);
-  }
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int i = 0; i < kStats; ++i) {
-#pragma unroll
-    for (int h = 0; h < 32; h += kBatch) {
-      const int x0 = 32 * i + h;
-      if (x0 >= n) break;
-      if (x0 > 0) load(x0);
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const float f = __shfl_sync(0xffffffffu, weight[i], h + k);
-        if (x0 + k < n) acc = make_float4(fmaf(f, v[k].x, acc.x), fmaf(f, v[k].y, acc.y), fmaf(f, v[k].z, acc.z), fmaf(f, v[k].w, acc.w));
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  write_row<E>(a, u, r, acc, top, sum, lane);
-}
-
 template <class E>
 __global__ void __launch_bounds__(E::kWarps * 32, E::kCtas)
 paged_attend_kernel(const __grid_constant__ Attend a) {
@@ -696,46 +541,11 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
   pdl_wait();
   pdl_trigger();
 
-  if (warp == 0) {
-    int64_t run = 0;
-    for (int b0 = 0; b0 < a.t.batch; b0 += 32) {
-      int units = 0, tiles = 0;
-      const int b = b0 + lane;
-      if (b < a.t.batch) {
-        const int held = a.pg.len[b];
-        tiles = tiles_of<E>(a, b, held, &units);
-        if (blockIdx.x == 0 && tiles > 0 && (int64_t)held + (a.t.cu[b + 1] - a.t.cu[b]) > (int64_t)a.pg.table_stride << a.pg.page_shift)
-          atomicOr(a.status, kStatusBadPage);
-      }
-      int64_t x = (int64_t)tiles * units;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
-      }
-      if (b < a.t.batch) before[b + 1] = run + x;
-      run += __shfl_sync(0xffffffffu, x, 31);
-    }
-    if (lane == 0) before[0] = 0;
-  }
+  if (warp == 0) count_tiles<E>(a, before, lane);
   __syncthreads();
-  // equal runs, of kMinRun tiles at least: below, a CTA more costs more (its part is written, and read by another) than it saves
-  const int64_t total = before[a.t.batch];
-  const int64_t ctas = max((int64_t)1, min((int64_t)gridDim.x, total / E::kMinRun));
-  if (blockIdx.x >= ctas) return;
-  const int64_t run_begin = total * blockIdx.x / ctas, run_end = total * (blockIdx.x + 1) / ctas;
-
+  Run run;
   Part c;
-  {
-    int lo = 0, hi = a.t.batch - 1, units;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (before[mid] <= run_begin) lo = mid; else hi = mid - 1;
-    }
-    const int tiles = tiles_of<E>(a, lo, a.pg.len[lo], &units);
-    const int unit = (int)((run_begin - before[lo]) / tiles);
-    place<E>(a, c, lo, unit, before[lo] + (int64_t)unit * tiles, run_begin, run_end);
-  }
+  if (!take_run<E>(a, before, run, c)) return;
 
   // Copies run kStages - 1 tiles ahead of the products, into the next units where these end.
   Part p = c;
@@ -779,7 +589,7 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
       }
       base_p += E::kTile;
       if (--left == 0) {
-        more = next<E>(a, p, before, run_end);
+        more = next<E>(a, p, before, run.end);
         if (more) enter();
       } else {
         look_up();
@@ -792,7 +602,7 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
 
   E e;
   int slot = 0, ahead = E::kStages - 1;
-  for (bool on = true; on; on = next<E>(a, c, before, run_end)) {
+  for (bool on = true; on; on = next<E>(a, c, before, run.end)) {
     e.begin(a, c.u, extra, warp, lane);
     int base = (int)(c.begin - c.unit_begin) * E::kTile + warp * (16 * E::kSub);
 #pragma unroll 1
@@ -811,10 +621,7 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
       slot = slot + 1 == E::kStages ? 0 : slot + 1;
     }
     // ---- the run leaves this unit
-    const int64_t unit_end = c.unit_begin + c.tiles;
-    const bool alone = c.unit_begin >= run_begin && unit_end <= run_end;
-    const int64_t c0 = ((c.unit_begin + 1) * ctas - 1) / total, c1 = (unit_end * ctas - 1) / total;
-    float* const part = a.part + (2 * (int64_t)blockIdx.x + (c.unit_begin > run_begin ? 1 : 0)) * kSlotFloats;
+    const Share<E> share(a, run, c);
     for (int nt = 0; nt < E::kNT; ++nt) {
       __syncthreads();
       e.flush(buf + warp * kBufRow, ml + warp * 8, nt, lane);
@@ -831,26 +638,23 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
           sum = fmaf(f, ml[w * 8 + r].y, sum);
           acc = make_float4(fmaf(f, x.x, acc.x), fmaf(f, x.y, acc.y), fmaf(f, x.z, acc.z), fmaf(f, x.w, acc.w));
         }
-        if (alone) {
+        if (share.alone) {
           write_row<E>(a, c.u, 8 * nt + r, acc, top, sum, lane);
         } else {
-          __stcg(reinterpret_cast<float4*>(part + (8 * nt + r) * kHeadDim) + lane, acc);
-          if (lane == 0) __stcg(reinterpret_cast<float2*>(part + kMaxRows * kHeadDim) + 8 * nt + r, make_float2(top, sum));
+          __stcg(reinterpret_cast<float4*>(share.mine + (8 * nt + r) * kHeadDim) + lane, acc);
+          if (lane == 0) __stcg(reinterpret_cast<float2*>(share.mine + E::kSlotRows * kHeadDim) + 8 * nt + r, make_float2(top, sum));
         }
       }
     }
-    if (!alone) {
+    if (!share.alone) {
       __threadfence();
       __syncthreads();
-      if (threadIdx.x == 0) last_here = atomicAdd(a.sync + c0, 1u) == (uint32_t)(c1 - c0);
+      if (threadIdx.x == 0) last_here = atomicAdd(a.sync + share.c0, 1u) == (uint32_t)(share.n - 1);
       __syncthreads();
       if (last_here) {
         __threadfence();
-        const bool inside = c.unit_begin > total * c0 / ctas;             // (the first CTA's part: behind another one of its own)
-        const float* first = a.part + (2 * c0 + (inside ? 1 : 0)) * kSlotFloats;
-        const int n = (int)(c1 - c0) + 1;
-        for (int r = warp; r < E::kRows; r += E::kWarps) merge_row<E>(a, c.u, r, first, a.part + 2 * c0 * kSlotFloats, n, lane);
-        if (threadIdx.x == 0) a.sync[c0] = 0u;
+        for (int r = warp; r < E::kRows; r += E::kWarps) merge_row<E>(a, c.u, r, share.first, share.others, share.n, lane);
+        if (threadIdx.x == 0) a.sync[share.c0] = 0u;
       }
     }
     __syncthreads();
@@ -863,30 +667,47 @@ cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
   constexpr int smem = E::kWarps * (E::kStages * E::kStageBytes + 8 * kPadRow * 4 + 64) + E::kExtra;
   cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  // no more CTAs than there can be tiles
-  int64_t most = 0;
-  const int64_t tiles = (((int64_t)a.pg.table_stride << a.pg.page_shift) + E::kTile - 1) / E::kTile;
-  for (int b = 0; b < a.t.batch; ++b) most += (int64_t)a.n_kv_heads * (((int64_t)(a.t.cu[b + 1] - a.t.cu[b]) * a.group + E::kRows - 1) / E::kRows) * tiles;
-  const int64_t grid = (int64_t)min(n_sm, kMostSms) * E::kCtas;
-  return launch_pdl(paged_attend_kernel<E>, dim3((unsigned)(most < grid ? most : grid)), dim3(E::kWarps * 32), smem, s, 1, a);
+  return launch_pdl(paged_attend_kernel<E>, dim3((unsigned)most_ctas<E>(a, n_sm)), dim3(E::kWarps * 32), smem, s, 1, a);
 }
 
 }  // namespace
 
-size_t attend_part_floats(int n_sm) { return (size_t)2 * min(n_sm, kMostSms) * kMaxCtasPerSm * kSlotFloats; }
-size_t attend_sync_words(int n_sm) { return (size_t)min(n_sm, kMostSms) * kMaxCtasPerSm; }
+// Query rows of a sequence and KV head up to which the kernels here take them; more go to the one that has them on the tall side of
+// tcgen05 tiles.
+constexpr int kFewRows = 16;
+
+size_t attend_part_floats(int n_sm, bool bf16) {
+  const size_t few = 2 * kSlotFloats<TensorEngine<true, 1>>, many = bf16 ? attend_many_part_floats() : 0;
+  return min(n_sm, kMostSms) * (2 * few > many ? 2 * few : many);
+}
+size_t attend_sync_words(int n_sm) { return (size_t)2 * min(n_sm, kMostSms); }
 
 cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t, const Dims& dm, const void* q, int64_t q_stride, float softcap, void* out,
-                                float* lse, float* part, uint32_t* sync, int n_sm, int* status, cudaStream_t s, LaunchLog* log) {
-  Attend a = {pg, t, q, q_stride, out, lse, part, sync, status, dm.n_q_heads, dm.n_kv_heads, dm.group, dm.scale_log2e, softcap};
-  int rows = 0;
-  for (int b = 0; b < t.batch; ++b) rows = max(rows, (t.cu[b + 1] - t.cu[b]) * dm.group);
-  log->begin(kKindPagedAttend, s);
-  cudaError_t e;
-  if (dtype == DAPQ_F32) e = pg.fp4 ? go<FloatEngine<true>>(a, n_sm, s) : go<FloatEngine<false>>(a, n_sm, s);
-  else if (rows <= 8) e = pg.fp4 ? go<TensorEngine<true, 1>>(a, n_sm, s) : go<TensorEngine<false, 1>>(a, n_sm, s);
-  else e = pg.fp4 ? go<TensorEngine<true, 2>>(a, n_sm, s) : go<TensorEngine<false, 2>>(a, n_sm, s);
-  log->end(s);
+                                float* lse, float* part, uint32_t* sync, int n_sm, int* status, long long wait_limit, cudaStream_t s, LaunchLog* log) {
+  Attend few = {pg, t.batch, {}, {}, q, q_stride, out, lse, part, sync, status, wait_limit, dm.n_q_heads, dm.n_kv_heads, dm.group, dm.scale_log2e, softcap};
+  Attend many = few;
+  int rows_few = 0, rows_many = 0;
+  for (int b = 0; b < t.batch; ++b) {
+    const int n = t.cu[b + 1] - t.cu[b], rows = n * dm.group;
+    const bool is_many = dtype == DAPQ_BF16 && rows > kFewRows;
+    (is_many ? rows_many : rows_few) = max(is_many ? rows_many : rows_few, rows);
+    few.start[b] = many.start[b] = t.cu[b];
+    few.n[b] = is_many ? 0 : n;
+    many.n[b] = is_many ? n : 0;
+  }
+  cudaError_t e = cudaSuccess;
+  if (rows_few > 0) {
+    log->begin(kKindPagedAttend, s);
+    if (dtype == DAPQ_F32) e = pg.fp4 ? go<FloatEngine<true>>(few, n_sm, s) : go<FloatEngine<false>>(few, n_sm, s);
+    else if (rows_few <= 8) e = pg.fp4 ? go<TensorEngine<true, 1>>(few, n_sm, s) : go<TensorEngine<false, 1>>(few, n_sm, s);
+    else e = pg.fp4 ? go<TensorEngine<true, 2>>(few, n_sm, s) : go<TensorEngine<false, 2>>(few, n_sm, s);
+    log->end(s);
+  }
+  if (rows_many > 0 && e == cudaSuccess) {
+    log->begin(kKindPagedAttend, s);
+    e = launch_attend_many(many, n_sm, s);
+    log->end(s);
+  }
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

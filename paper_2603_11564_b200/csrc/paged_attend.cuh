@@ -1,0 +1,246 @@
+// What the attention kernels over the paged cache share: how the work is numbered and dealt out, and how partial results are joined.
+//
+// Work: (sequence, KV head, query row tile, key tile), numbered in this order.  Lengths are known on the device only, so every CTA of one
+// wave adds them up and takes an equal run of the numbers, whatever the lengths are.  A CTA's result for a unit (sequence, head,
+// row tile) is final if its run covers the unit; otherwise it goes to the workspace, and the last of the unit's CTAs to arrive
+// joins their results in CTA order, so that the result does not depend on who that is.  Nobody waits for another CTA.
+//
+// Softmax: base 2, against a maximum that is only moved when a logit exceeds it by more than kSlack.
+#pragma once
+#include "paged.cuh"
+#include "umma_ptx.cuh"
+
+namespace dapq {
+
+struct Attend {
+  PagedDev pg;
+  int32_t batch;
+  int32_t start[kMaxBatch], n[kMaxBatch];            // first new token of each sequence, and how many; 0: not in this launch
+  const void* q;
+  int64_t q_stride;
+  void* out;
+  float *lse, *part;
+  uint32_t* sync;
+  int* status;
+  long long wait_limit;
+  int32_t n_q_heads, n_kv_heads, group;
+  float scale_log2e, softcap;
+};
+
+// The kernel for many query rows (paged_attend_many.cu), and what its partial results take per CTA.
+cudaError_t launch_attend_many(const Attend& a, int n_sm, cudaStream_t s);
+size_t attend_many_part_floats();
+
+namespace {
+
+using ptx::ex2;
+using ptx::smem_u32;
+
+constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
+constexpr int kMostSms = 160;                        // (more SMs than that: one wave on 160 of them)
+
+// c tanh(x / c) log2(e) of x = y c / (2 log2(e)), through the exponential (the tanh instruction has 11 bits).
+__device__ __forceinline__ float capped(float y, float c_log2e) { return c_log2e - __fdividef(2.f * c_log2e, 1.f + ex2(y)); }
+
+// What a unit is: a row tile of one sequence and KV head.
+struct Unit {
+  int b, h, row0;          // first query row; row r is query r / group of the sequence, head h * group + r % group
+  int rows;                // rows of the sequence
+  int held, limit;         // rows held before the step, end of the rows that any of the tile's queries sees
+  int full;                // end of the rows that all of them see
+};
+
+// Tiles of a sequence's units, and their number.
+template <class E>
+__device__ __forceinline__ int tiles_of(const Attend& a, int b, int held, int* units) {
+  const int n = a.n[b];
+  *units = a.n_kv_heads * ((n * a.group + E::kRows - 1) / E::kRows);
+  const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift, rows = held < 0 ? 0 : min((int64_t)held + n, room);
+  return n == 0 ? 0 : max(1, (int)((rows + E::kTile - 1) / E::kTile));
+}
+
+// A part of a CTA's run of tiles that lies in one unit.
+struct Part {
+  int64_t begin, end, unit_begin;                    // tiles of the call: [begin, end) of the unit's [unit_begin, unit_begin + tiles)
+  int tiles, unit;                                   // of the sequence u.b
+  Unit u;
+};
+
+template <class E>
+__device__ __forceinline__ void place(const Attend& a, Part& p, int b, int unit, int64_t unit_begin, int64_t begin, int64_t run_end) {
+  const int n = a.n[b], held = a.pg.len[b];
+  int units;
+  p.tiles = tiles_of<E>(a, b, held, &units);
+  p.unit = unit;
+  p.unit_begin = unit_begin;
+  p.begin = begin;
+  p.end = min(run_end, unit_begin + p.tiles);
+  Unit& u = p.u;
+  u.b = b;
+  u.rows = n * a.group;
+  const int row_tiles = units / a.n_kv_heads;
+  u.h = unit / row_tiles;
+  u.row0 = (unit - u.h * row_tiles) * E::kRows;
+  u.held = held;
+  const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift;
+  const int first = u.row0 / a.group, last = min((u.row0 + E::kRows - 1) / a.group, n - 1);
+  u.limit = held < 0 ? 0 : (int)min((int64_t)held + last + 1, room);
+  u.full = held < 0 ? 0 : (int)min((int64_t)held + first + 1, room);
+}
+// The part of the run behind p, if there is one.
+template <class E>
+__device__ __forceinline__ bool next(const Attend& a, Part& p, const int64_t* before, int64_t run_end) {
+  if (p.end >= run_end) {
+    p.begin = p.end;
+    return false;
+  }
+  const int64_t at = p.end;                          // (the part ended with its unit)
+  int b = p.u.b, unit = p.unit + 1;
+  if (at >= before[b + 1]) {
+    unit = 0;
+    do ++b; while (before[b + 1] <= at);
+  }
+  place<E>(a, p, b, unit, at, at, run_end);
+  return true;
+}
+// Rows that query row r of the unit sees.
+__device__ __forceinline__ int sees(const Attend& a, const Unit& u, int r) {
+  const int row = u.row0 + r;
+  return row < u.rows && u.held >= 0 ? (int)min((int64_t)u.held + row / a.group + 1, (int64_t)u.limit) : 0;
+}
+
+// Slot s of the workspace: [E::kSlotRows][128] outputs, then their maxima and sums.  A CTA has two, for the units that its run begins
+// and ends within.
+template <class E>
+constexpr int64_t kSlotFloats = (int64_t)E::kSlotRows * (kHeadDim + 2);
+
+__device__ __forceinline__ void store2(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
+__device__ __forceinline__ void store2(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
+
+// Positions 4 lane .. 4 lane + 3 of row r of the unit, weights summing to `sum` against the maximum `top`.
+template <class E>
+__device__ __forceinline__ void write_row(const Attend& a, const Unit& u, int r, float4 acc, float top, float sum, int lane) {
+  const int row = u.row0 + r;
+  if (row >= u.rows) return;
+  const int i = row / a.group, h = u.h * a.group + row - i * a.group;
+  const int64_t at = (int64_t)(a.start[u.b] + i) * a.n_q_heads + h;
+  const float f = sum == 0.f ? 0.f : (a.pg.fp4 ? a.pg.v_scale : 1.f) / sum;
+  typename E::T* out = (typename E::T*)a.out + at * kHeadDim;
+  store2(out + E::channel(4 * lane), acc.x * f, acc.y * f);
+  store2(out + E::channel(4 * lane + 2), acc.z * f, acc.w * f);
+  if (a.lse != nullptr && lane == 0) a.lse[at] = sum == 0.f ? -CUDART_INF_F : (top - E::kLift + log2f(sum)) * 0.69314718f;
+}
+
+// Row r of a unit from the partial results of n CTAs, in their order: the first one's at `first`, the x-th one's at others + 2 x slots.  What a
+// warp waits for is latency, so its loads are in flight together: all maxima and sums, and kBatch outputs at a time.
+template <class E>
+__device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r, const float* first, const float* others, int n, int lane) {
+  constexpr int kBatch = 16;
+  auto from = [&](int x) { return x == 0 ? first : others + 2 * (int64_t)x * kSlotFloats<E>; };
+  auto stats = [&](int x) {
+    return x < n ? __ldcg(reinterpret_cast<const float2*>(from(x) + E::kSlotRows * kHeadDim) + r) : make_float2(kLowest, 0.f);
+  };
+  const float2 st0 = stats(lane), st1 = stats(32 + lane);
+  float top = fmaxf(st0.x, st1.x), sum = 0.f;
+  for (int x = 64 + lane; x < n; x += 32) top = fmaxf(top, stats(x).x);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int x0 = 0; x0 < n; x0 += 32) {
+    const float2 st = x0 == 0 ? st0 : x0 == 32 ? st1 : stats(x0 + lane);
+    const float weight = x0 + lane < n ? ex2(st.x - top) : 0.f;
+    sum = fmaf(weight, st.y, sum);
+#pragma unroll 1
+    for (int h = 0; h < min(32, n - x0); h += kBatch) {
+      float4 v[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(from(min(x0 + h + i, n - 1)) + r * kHeadDim) + lane);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const float f = __shfl_sync(0xffffffffu, weight, (h + i) & 31);
+        if (x0 + h + i < n) acc = make_float4(fmaf(f, v[i].x, acc.x), fmaf(f, v[i].y, acc.y), fmaf(f, v[i].z, acc.z), fmaf(f, v[i].w, acc.w));
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  write_row<E>(a, u, r, acc, top, sum, lane);
+}
+
+
+// Tiles before each sequence, by one warp.
+template <class E>
+__device__ __forceinline__ void count_tiles(const Attend& a, int64_t* before, int lane) {
+  int64_t run = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    int units = 0, tiles = 0;
+    const int b = b0 + lane;
+    if (b < a.batch) {
+      const int held = a.pg.len[b];
+      tiles = tiles_of<E>(a, b, held, &units);
+      if (blockIdx.x == 0 && tiles > 0 && (int64_t)held + a.n[b] > (int64_t)a.pg.table_stride << a.pg.page_shift) atomicOr(a.status, kStatusBadPage);
+    }
+    int64_t x = (int64_t)tiles * units;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
+    }
+    if (b < a.batch) before[b + 1] = run + x;
+    run += __shfl_sync(0xffffffffu, x, 31);
+  }
+  if (lane == 0) before[0] = 0;
+}
+
+// A CTA's run, and its first part.  Runs are equal, and of kMinRun tiles at least: below that, a CTA more costs more (its part is written,
+// and read by another) than it saves.
+struct Run {
+  int64_t total, ctas, begin, end;
+};
+template <class E>
+__device__ __forceinline__ bool take_run(const Attend& a, const int64_t* before, Run& run, Part& c) {
+  run.total = before[a.batch];
+  run.ctas = max((int64_t)1, min((int64_t)gridDim.x, run.total / E::kMinRun));
+  if (blockIdx.x >= run.ctas) return false;
+  run.begin = run.total * blockIdx.x / run.ctas;
+  run.end = run.total * (blockIdx.x + 1) / run.ctas;
+  int lo = 0, hi = a.batch - 1, units;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (before[mid] <= run.begin) lo = mid; else hi = mid - 1;
+  }
+  const int tiles = tiles_of<E>(a, lo, a.pg.len[lo], &units);
+  const int unit = (int)((run.begin - before[lo]) / tiles);
+  place<E>(a, c, lo, unit, before[lo] + (int64_t)unit * tiles, run.begin, run.end);
+  return true;
+}
+// Whether the run covers a part's whole unit; else the CTAs that share it, and this one's slot.
+template <class E>
+struct Share {
+  bool alone;
+  int64_t c0;
+  int n;
+  float *mine, *first, *others;
+  __device__ __forceinline__ Share(const Attend& a, const Run& run, const Part& c) {
+    const int64_t unit_end = c.unit_begin + c.tiles;
+    alone = c.unit_begin >= run.begin && unit_end <= run.end;
+    c0 = ((c.unit_begin + 1) * run.ctas - 1) / run.total;
+    n = (int)((unit_end * run.ctas - 1) / run.total - c0) + 1;
+    mine = a.part + (2 * (int64_t)blockIdx.x + (c.unit_begin > run.begin ? 1 : 0)) * kSlotFloats<E>;
+    others = a.part + 2 * c0 * kSlotFloats<E>;
+    first = others + (c.unit_begin > run.total * c0 / run.ctas ? kSlotFloats<E> : 0);     // (behind another one of that CTA's own)
+  }
+};
+// No more CTAs than there can be tiles.
+template <class E>
+int64_t most_ctas(const Attend& a, int n_sm) {
+  int64_t most = 0;
+  const int64_t tiles = (((int64_t)a.pg.table_stride << a.pg.page_shift) + E::kTile - 1) / E::kTile;
+  for (int b = 0; b < a.batch; ++b) most += (int64_t)a.n_kv_heads * (((int64_t)a.n[b] * a.group + E::kRows - 1) / E::kRows) * tiles;
+  const int64_t grid = (int64_t)(n_sm < kMostSms ? n_sm : kMostSms) * E::kCtas;
+  return most < grid ? most : grid;
+}
+
+}  // namespace
+}  // namespace dapq

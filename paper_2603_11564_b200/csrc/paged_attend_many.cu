@@ -1,0 +1,495 @@
+// Attention over the paged cache for many query rows of a sequence and KV head (a chunk of new tokens): rows on the tall side of tcgen05
+// tiles, 4 n L H_q d flops against one reading of the cache per 256 rows.
+//
+// A CTA has two tiles of 128 query rows (A and B) over the same keys, 128 at a time.  Four warps bring keys and values to shared memory as
+// 16-bit tiles with the 128-byte swizzle (codes times scales where the cache has 4 bits: done once for 256 query rows); one thread
+// issues the MMAs; four warps a tile take the softmax, one row a thread.  S = Q K^T goes to tensor memory, is read whole by its row's thread,
+// and comes back as the weights P, 16-bit, in the same columns, from where the second MMA takes them as its left operand; O += P V stays
+// in tensor memory.  V's tile is the right operand with its keys down (MN-major), so nothing is transposed.  While a tile's
+// rows are exponentiated the tensor cores have the other tile's two products: 4 x 128^3 a step, some 2800 cycles, against 2 x 128^2
+// exponentials, 2048 cycles of the MUFU.
+//
+// Types as in paged_attend.cu: fp16 for 4-bit caches (keys, values exact; queries exact after a power of two a row; weights, 2^11 times what
+// they are, to 11 bits), bf16 for bf16 caches (weights to 8 bits).
+#include "paged_attend.cuh"
+
+namespace dapq {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 512;
+constexpr int kHalfTile = 128 * 128;                  // bytes of 64 channels of 128 rows
+constexpr int kTileBytes = 2 * kHalfTile;
+constexpr int kRing = 2;                              // tiles of K, and of V, in shared memory
+struct Smem {
+  static constexpr int q = 0, k = 2 * kTileBytes, v = k + kRing * kTileBytes, bars = v + kRing * kTileBytes;
+  // barriers
+  static constexpr int k_full = 0, k_empty = 2, v_full = 4, v_empty = 6, q_full = 8, s_full = 10, p_full = 12, pv_done = 14, drain = 16, n_bars = 17;
+  static constexpr int before = bars + 8 * n_bars, tmem_ptr = before + 8 * (kMaxBatch + 1), abort_flag = tmem_ptr + 4, last_here = abort_flag + 4,
+                       total = last_here + 4;
+};
+static_assert(Smem::total <= 232448, "exceeds the shared memory a CTA can opt in to");
+
+struct Many {                                         // geometry, for the shared scheduling
+  static constexpr int kRows = 256, kSlotRows = 256, kTile = 128, kCtas = 1, kMinRun = 4;
+  using T = __nv_bfloat16;
+  __device__ __forceinline__ static int channel(int p) { return p; }
+};
+template <bool kFp4> struct ManyOf : Many { static constexpr float kLift = kFp4 ? 11.f : 0.f; };
+
+// D (tensor memory) (+)= A (tensor memory) B (shared memory)
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The right operand of the second product: 64-channel halves of 128-byte rows like umma_desc's, but the contraction runs down the rows:
+// groups of 8 rows 1024 bytes apart, halves of the channels kHalfTile apart.
+__device__ __forceinline__ uint64_t values_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3ffffu) >> 4) | ((uint64_t)(kHalfTile >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ uint32_t pack(bool f16, float x, float y) {
+  if (f16) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+struct Wait {
+  uint32_t bars;
+  volatile int* abort_flag;
+  int* status;
+  long long limit;
+  __device__ __forceinline__ uint32_t bar(int i) const { return bars + 8u * i; }
+  __device__ __forceinline__ bool operator()(int i, uint32_t parity) const { return mbar_wait_limit(bar(i), parity, abort_flag, status, limit); }
+  __device__ __forceinline__ bool warp(int i, uint32_t parity) const { return __all_sync(0xffffffffu, (*this)(i, parity)); }
+};
+
+// The 16-row pieces of a tile: lane p < 8 looks up the page of keys base + 16 p (a tile ahead of its use; -1 behind the limit).
+__device__ __forceinline__ int tile_page(const Attend& a, const Unit& u, int base, int lane) {
+  const int row = base + 16 * lane;
+  return lane < 8 && row < u.limit ? __ldg(a.pg.table + (int64_t)u.b * a.pg.table_stride + (row >> a.pg.page_shift)) : -1;
+}
+
+// ---- keys and values to shared memory -------------------------------------------------------------------------------------
+struct Codes { uint4 w[4]; uint2 scales; };
+__device__ __forceinline__ Codes load_codes(const char* codes, const unsigned char* scales, int64_t off) {
+  Codes c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c.w[i] = off < 0 ? make_uint4(0, 0, 0, 0) : __ldg(reinterpret_cast<const uint4*>(codes + (off >> 1)) + i);
+  c.scales = off < 0 ? make_uint2(0, 0) : __ldg(reinterpret_cast<const uint2*>(scales + (off >> 4)));
+  return c;
+}
+// Row r of a tile at `tile`: 16 pieces of 16 bytes.
+__device__ __forceinline__ uint32_t piece(uint32_t tile, int r, int c) { return tile + (c >> 3) * kHalfTile + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+__device__ __forceinline__ void store_codes(uint32_t tile, int r, const Codes& c) {
+  const uint32_t s[4] = {scales_to_half(c.scales.x), scales_to_half(c.scales.x >> 16), scales_to_half(c.scales.y), scales_to_half(c.scales.y >> 16)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w[4] = {c.w[i].x, c.w[i].y, c.w[i].z, c.w[i].w};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {                                         // 8 channels; a scale for two of these
+      const __half2 two = *reinterpret_cast<const __half2*>(&s[i]), f = x < 2 ? __low2half2(two) : __high2half2(two);
+      uint32_t h[4];
+      codes_to_half(w[x], h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[e]), f);
+        h[e] = *reinterpret_cast<const uint32_t*>(&y);
+      }
+      sts128(piece(tile, r, 4 * i + x), make_uint4(h[0], h[1], h[2], h[3]));
+    }
+  }
+}
+
+template <bool kFp4>
+__device__ __forceinline__ void produce(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint32_t sbase) {
+  const int tid = threadIdx.x - 256, lane = tid & 31, warp = tid >> 5;
+  int done = 0;                                                           // tiles so far
+  for (bool on = true; on; on = next<Many>(a, c, before, run.end)) {
+    const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile;
+    int page = tile_page(a, c.u, first, lane), ahead = 0;
+    for (int i = 0; i < n; ++i, ++done, page = ahead) {
+      const int base = first + i * Many::kTile, st = done & 1;
+      const bool sound = (unsigned)page < (unsigned)a.pg.n_pages;
+      if (warp == 0 && lane < 8 && base + 16 * lane < c.u.limit && !sound) atomicOr(a.status, kStatusBadPage);
+      if (i + 1 < n) ahead = tile_page(a, c.u, base + Many::kTile, lane);
+      auto offset = [&](int r) {                                          // channel offset of row r of the tile, negative: reads as zero
+        const int pg = __shfl_sync(0xffffffffu, sound ? page : -1, r >> 4);
+        return pg < 0 || base + r >= c.u.limit
+                   ? (int64_t)-1
+                   : pg * a.pg.page_stride + c.u.h * a.pg.head_stride + (int64_t)((base + r) & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride;
+      };
+      const uint32_t parity = ((done >> 1) & 1) ^ 1;
+      if constexpr (kFp4) {
+        const int64_t off = offset(tid);
+        const Codes k = load_codes(a.pg.k, a.pg.k_scales, off), v = load_codes(a.pg.v, a.pg.v_scales, off);
+        if (done >= kRing && !wait.warp(Smem::k_empty + st, parity)) return;
+        store_codes(sbase + Smem::k + st * kTileBytes, tid, k);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(wait.bar(Smem::k_full + st));
+        if (done >= kRing && !wait.warp(Smem::v_empty + st, parity)) return;
+        store_codes(sbase + Smem::v + st * kTileBytes, tid, v);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(wait.bar(Smem::v_full + st));
+      } else {
+        auto copy = [&](uint32_t tile, const char* from) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int r = 8 * j + (tid >> 4);
+            const int64_t off = offset(r);
+            const uint32_t to = piece(tile, r, tid & 15);
+            if (off < 0) sts128(to, make_uint4(0, 0, 0, 0));
+            else cp_async16(to, from + 2 * off + (tid & 15) * 16);
+          }
+          cp_async_commit();
+        };
+        if (done >= kRing && !wait.warp(Smem::k_empty + st, parity)) { cp_async_wait<0>(); return; }
+        copy(sbase + Smem::k + st * kTileBytes, a.pg.k);
+        if (done >= kRing && !wait.warp(Smem::v_empty + st, parity)) { cp_async_wait<0>(); return; }
+        copy(sbase + Smem::v + st * kTileBytes, a.pg.v);
+        cp_async_wait<1>();
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(wait.bar(Smem::k_full + st));
+        cp_async_wait<0>();
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(wait.bar(Smem::v_full + st));
+      }
+    }
+  }
+}
+
+// ---- the MMAs ---------------------------------------------------------------------------------------------------------------
+template <bool kFp4>
+__device__ __forceinline__ void issue(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint32_t sbase, uint32_t tmem) {
+  const uint32_t idesc_s = kFp4 ? umma_idesc_f16(128, 128) : umma_idesc(128, 128), idesc_o = idesc_s | (1u << 16);   // (V: MN-major)
+  int done = 0, parts = 0, parts_b = 0, done_b = 0;
+  bool ok = true;
+  auto scores = [&](int x, int st) {                                      // S of tile x
+    const uint64_t q = umma_desc(sbase + Smem::q + x * kTileBytes), k = umma_desc(sbase + Smem::k + st * kTileBytes);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+      umma_ss(tmem + x * 128, desc_advance(q, (ks >> 2) * kHalfTile + (ks & 3) * 32), desc_advance(k, (ks >> 2) * kHalfTile + (ks & 3) * 32), idesc_s, ks ? 1u : 0u);
+    tc_commit(wait.bar(Smem::s_full + x));
+  };
+  auto outputs = [&](int x, int st, bool more) {                          // O of tile x
+    const uint64_t v = values_desc(sbase + Smem::v + st * kTileBytes);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) umma_ts(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, desc_advance(v, ks * 2048), idesc_o, more || ks ? 1u : 0u);
+    tc_commit(wait.bar(Smem::pv_done + x));
+  };
+  for (bool on = true; on && ok; on = next<Many>(a, c, before, run.end)) {
+    const int n = (int)(c.end - c.begin);
+    const bool two = c.u.rows - c.u.row0 > 128;
+    ok = wait(Smem::q_full, parts & 1) && (!two || wait(Smem::q_full + 1, parts_b & 1)) && wait(Smem::k_full + (done & 1), (done >> 1) & 1);
+    if (!ok) break;
+    tc_fence_after();
+    scores(0, done & 1);
+    if (two) scores(1, done & 1);
+    tc_commit(wait.bar(Smem::k_empty + (done & 1)));
+    for (int i = 0; i < n && ok; ++i) {
+      const int t = done + i, st = t & 1, st1 = st ^ 1;
+      ok = wait(Smem::v_full + st, (t >> 1) & 1);
+      if (ok && i + 1 < n) ok = wait(Smem::k_full + st1, ((t + 1) >> 1) & 1);
+      for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
+        ok = wait(Smem::p_full + x, (x ? done_b + i : t) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        outputs(x, st, i > 0);
+        if (i + 1 < n) scores(x, st1);
+      }
+      tc_commit(wait.bar(Smem::v_empty + st));
+      if (i + 1 < n) tc_commit(wait.bar(Smem::k_empty + st1));
+    }
+    done += n;
+    ++parts;
+    if (two) {
+      done_b += n;
+      ++parts_b;
+    }
+  }
+  if (!ok) {                                                              // see what was issued retire before tensor memory goes
+    tc_commit(wait.bar(Smem::drain));
+    drain_wait(wait.bar(Smem::drain), 0, kWaitLimit);
+  }
+}
+
+// ---- the softmax ------------------------------------------------------------------------------------------------------------
+template <bool kFp4>
+__device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint8_t* smem, uint32_t sbase,
+                                        uint32_t tmem) {
+  using E = ManyOf<kFp4>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = warp >> 2, r = threadIdx.x & 127;
+  const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, ts = tmem + lanes + x * 128, to = ts + 256;
+  volatile int* last_here = reinterpret_cast<volatile int*>(smem + Smem::last_here);
+  int done = 0;                                                           // tiles of this half so far
+  bool ok = true;
+  // (an aborting warp still walks every part: the others wait for it at the barriers, and the arrival counters have to come back to 0)
+  for (bool on = true; on; on = next<Many>(a, c, before, run.end)) {
+    const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile, row = c.u.row0 + x * 128 + r;
+    const bool mine = x == 0 || c.u.rows - c.u.row0 > 128;                // (tile B of a unit of 128 rows or fewer has none)
+    float m = kLowest, l = 0.f;
+    if (mine) {
+      // the row's query to shared memory
+      uint4 w[16] = {};
+      if (row < c.u.rows) {
+        const int i = row / a.group, h = c.u.h * a.group + row - i * a.group;
+        const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (int64_t)(a.start[c.u.b] + i) * a.q_stride + h * kHeadDim);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w[j] = __ldg(src + j);
+      }
+      float f = a.scale_log2e;
+      if (kFp4) {
+        uint32_t* raw = reinterpret_cast<uint32_t*>(w);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) top = max(top, max((raw[i] << 16) & 0x7fffffffu, raw[i] & 0x7fff0000u));
+        const int e = top == 0 ? 127 : min(max((int)(top >> 23), 1), 253);
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < 64; ++i) raw[i] = pack(true, __uint_as_float(raw[i] << 16) * down, __uint_as_float(raw[i] & 0xffff0000u) * down);
+        f *= __uint_as_float((uint32_t)e << 23) * a.pg.k_scale;
+      }
+      if (a.softcap > 0.f) f *= 2.f / a.softcap;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) sts128(piece(sbase + Smem::q + x * kTileBytes, r, j), w[j]);
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(wait.bar(Smem::q_full + x));
+
+      const int lim = sees(a, c.u, x * 128 + r);
+      int page = tile_page(a, c.u, first, lane), ahead = 0;
+      for (int i = 0; i < n && ok; ++i, ++done, page = ahead) {
+        const int base = first + i * Many::kTile;
+        const uint32_t gone = __ballot_sync(0xffffffffu, lane < 8 && (unsigned)page >= (unsigned)a.pg.n_pages);   // (pieces behind the limit too)
+        if (i + 1 < n) ahead = tile_page(a, c.u, base + Many::kTile, lane);
+        ok = wait.warp(Smem::s_full + x, done & 1);
+        if (!ok) break;
+        tc_fence_after();
+        // twice over the row, 32 columns at a time (the next ones on their way): its maximum, then its weights.  To hold all 128 took
+        // more registers than a softmax warp can have.
+        const bool masked = base + Many::kTile > c.u.full || gone;
+        uint32_t s[2][32];
+        auto hide = [&](uint32_t (&v)[32], int p) {
+          if (masked) {
+            const int left = (gone >> (2 * p)) & 1u ? 0 : (gone >> (2 * p + 1)) & 1u ? min(lim - base - 32 * p, 16) : lim - base - 32 * p;
+            const bool second = ((gone >> (2 * p)) & 3u) == 1u;           // (the first 16 of the 32 gone, the others there)
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (second ? j < 16 || base + 32 * p + j >= lim : j >= left) v[j] = 0xff800000u;
+          }
+        };
+        float t0 = -CUDART_INF_F, t1 = -CUDART_INF_F;
+        tmem_ld32(ts, s[0]);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          tmem_ld_wait_for(s[p & 1]);
+          tmem_ld32(ts + 32 * ((p + 1) & 3), s[(p + 1) & 1]);             // (behind the last: the first again)
+          hide(s[p & 1], p);
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            t0 = max3(t0, __uint_as_float(s[p & 1][j]), __uint_as_float(s[p & 1][j + 1]));
+            t1 = max3(t1, __uint_as_float(s[p & 1][j + 2]), __uint_as_float(s[p & 1][j + 3]));
+          }
+        }
+        tmem_ld_wait_for(s[0]);
+        float top = fmaxf(t0, t1) * f, g = f;
+        if (a.softcap > 0.f) {
+          top = top == -CUDART_INF_F ? top : capped(top, a.softcap * 1.44269504f);      // (the cap keeps the order)
+          g = 1.f;
+        }
+        if (__any_sync(0xffffffffu, top > m + kSlack)) {
+          const float now = fmaxf(m, top), alpha = ex2(m - now);
+          m = now;
+          l *= alpha;
+          if (i > 0) {                                                    // (the first product of a part starts O anew)
+            ok = wait.warp(Smem::pv_done + x, (done - 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int p = 0; p < 8; ++p) {
+              uint32_t o[16];
+              tmem_ld16(to + 16 * p, o);
+              tmem_ld_wait_for16(o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * alpha);
+              tmem_st16(to + 16 * p, o);
+            }
+            tmem_st_wait();
+          }
+        }
+        const float2 g2 = make_float2(g, g), off = make_float2(E::kLift - m, E::kLift - m);
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          uint32_t (&v)[32] = s[p & 1];
+          if (p > 0) tmem_ld_wait_for(v);
+          if (p < 3) tmem_ld32(ts + 32 * (p + 1), s[(p + 1) & 1]);
+          if (a.softcap > 0.f) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(capped(__uint_as_float(v[j]) * f, a.softcap * 1.44269504f));
+          }
+          hide(v, p);
+          uint32_t pk[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float2 w = ex2_pair_mufu(__ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), g2, off));
+            sum = __fadd2_rn(sum, w);
+            pk[j] = pack(kFp4, w.x, w.y);
+          }
+          tmem_st16(ts + 16 * p, pk);                                     // (columns that have been read)
+        }
+        l += sum.x + sum.y;
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(wait.bar(Smem::p_full + x));
+      }
+      if (ok) ok = wait.warp(Smem::pv_done + x, (done - 1) & 1);
+      if (ok) {
+        const Share<E> share(a, run, c);
+        tc_fence_after();
+        const bool out = row < c.u.rows;
+        const int i = row / a.group, h = c.u.h * a.group + row - i * a.group;
+        const int64_t at = (int64_t)(a.start[c.u.b] + i) * a.n_q_heads + h;
+        const float down = l == 0.f ? 0.f : (kFp4 ? a.pg.v_scale : 1.f) / l;
+        __nv_bfloat16* dst = (__nv_bfloat16*)a.out + at * kHeadDim;
+        float* part = share.mine + (x * 128 + r) * kHeadDim;
+#pragma unroll 1
+        for (int p = 0; p < 4; ++p) {
+          uint32_t o[32];
+          tmem_ld32(to + 32 * p, o);
+          tmem_ld_wait_for(o);
+          // (a row that saw nothing has weights 0, and its sums may be 0 times an infinity that others see: its output is 0)
+          if (!out) continue;
+          if (share.alone) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+              uint32_t y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                y[e] = l == 0.f ? 0u : pack(false, __uint_as_float(o[j + 2 * e]) * down, __uint_as_float(o[j + 2 * e + 1]) * down);
+              *reinterpret_cast<uint4*>(dst + 32 * p + j) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) __stcg(reinterpret_cast<uint4*>(part + 32 * p + j), make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+          }
+        }
+        if (out && share.alone && a.lse != nullptr) a.lse[at] = l == 0.f ? -CUDART_INF_F : (m - E::kLift + log2f(l)) * 0.69314718f;
+        if (!share.alone) __stcg(reinterpret_cast<float2*>(share.mine + Many::kSlotRows * kHeadDim) + x * 128 + r, make_float2(m, l));
+        tc_fence_before();
+      }
+    }
+    const Share<E> share(a, run, c);
+    if (!share.alone) {
+      __threadfence();
+      softmax_sync();
+      if (threadIdx.x == 0) *last_here = atomicAdd(a.sync + share.c0, 1u) == (uint32_t)(share.n - 1);
+      softmax_sync();
+      if (*last_here) {
+        __threadfence();
+        for (int y = warp; y < Many::kRows && c.u.row0 + y < c.u.rows; y += 8) merge_row<E>(a, c.u, y, share.first, share.others, share.n, lane);
+        if (threadIdx.x == 0) a.sync[share.c0] = 0u;
+      }
+      softmax_sync();
+    }
+  }
+}
+
+template <bool kFp4>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_attend_many_kernel(const __grid_constant__ Attend a) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  if (sbase & 1023u) {                                                    // (uniform over the CTA: nothing has been set up yet)
+    if (threadIdx.x == 0) atomicOr(a.status, kStatusSmemAlign);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int64_t* const before = reinterpret_cast<int64_t*>(smem + Smem::before);
+  const Wait wait{sbase + Smem::bars, reinterpret_cast<volatile int*>(smem + Smem::abort_flag), a.status, a.wait_limit};
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Smem::n_bars; ++i) {
+      const bool four = i < Smem::k_empty || i == Smem::v_full || i == Smem::v_full + 1 || (i >= Smem::q_full && i < Smem::s_full) ||
+                        (i >= Smem::p_full && i < Smem::pv_done);
+      mbar_init(wait.bar(i), four ? 4 : 1);                               // the warps of a role, or the issuer's commit
+    }
+    *wait.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + Smem::tmem_ptr), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  pdl_wait();
+  pdl_trigger();
+  if (warp == 0) count_tiles<Many>(a, before, lane);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + Smem::tmem_ptr);
+  Run run;
+  Part c;
+  if (take_run<Many>(a, before, run, c)) {
+    if (warp < 8) {
+      softmax<kFp4>(a, c, before, run, wait, smem, sbase, tmem);
+    } else if (warp < 12) {
+      produce<kFp4>(a, c, before, run, wait, sbase);
+    } else {
+      if (warp == 12 && lane == 0) issue<kFp4>(a, c, before, run, wait, sbase, tmem);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+template <bool kFp4>
+cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
+  cudaError_t e = cudaFuncSetAttribute(paged_attend_many_kernel<kFp4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::total);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(paged_attend_many_kernel<kFp4>, dim3((unsigned)most_ctas<Many>(a, n_sm)), dim3(kThreads), Smem::total, s, 1, a);
+}
+
+}  // namespace
+
+size_t attend_many_part_floats() { return 2 * (size_t)kSlotFloats<Many>; }
+
+cudaError_t launch_attend_many(const Attend& in, int n_sm, cudaStream_t s) {
+  Attend a = in;
+  if (a.wait_limit <= 0) a.wait_limit = ptx::kWaitLimit;
+  return a.pg.fp4 ? go<true>(a, n_sm, s) : go<false>(a, n_sm, s);
+}
+
+}  // namespace dapq

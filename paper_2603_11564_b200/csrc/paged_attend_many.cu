@@ -129,31 +129,36 @@ template <bool kFp4>
 __device__ __forceinline__ void produce(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint32_t sbase) {
   const int tid = threadIdx.x - 256, lane = tid & 31, warp = tid >> 5;
   int done = 0;                                                           // tiles so far
+  Codes kc;
   for (bool on = true; on; on = next<Many>(a, c, before, run.end)) {
     const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile;
     int page = tile_page(a, c.u, first, lane), ahead = 0;
+    auto offset_of = [&](int pages, int base, int r) {                    // channel offset of row r of a tile, negative: reads as zero
+      const int pg = __shfl_sync(0xffffffffu, pages, r >> 4);
+      return (unsigned)pg >= (unsigned)a.pg.n_pages || base + r >= c.u.limit
+                 ? (int64_t)-1
+                 : pg * a.pg.page_stride + c.u.h * a.pg.head_stride + (int64_t)((base + r) & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride;
+    };
     for (int i = 0; i < n; ++i, ++done, page = ahead) {
       const int base = first + i * Many::kTile, st = done & 1;
       const bool sound = (unsigned)page < (unsigned)a.pg.n_pages;
       if (warp == 0 && lane < 8 && base + 16 * lane < c.u.limit && !sound) atomicOr(a.status, kStatusBadPage);
       if (i + 1 < n) ahead = tile_page(a, c.u, base + Many::kTile, lane);
-      auto offset = [&](int r) {                                          // channel offset of row r of the tile, negative: reads as zero
-        const int pg = __shfl_sync(0xffffffffu, sound ? page : -1, r >> 4);
-        return pg < 0 || base + r >= c.u.limit
-                   ? (int64_t)-1
-                   : pg * a.pg.page_stride + c.u.h * a.pg.head_stride + (int64_t)((base + r) & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride;
-      };
+      auto offset = [&](int r) { return offset_of(page, base, r); };
       const uint32_t parity = ((done >> 1) & 1) ^ 1;
       if constexpr (kFp4) {
+        // (a row's codes are on their way while those before them are turned into operands)
         const int64_t off = offset(tid);
-        const Codes k = load_codes(a.pg.k, a.pg.k_scales, off), v = load_codes(a.pg.v, a.pg.v_scales, off);
+        if (i == 0) kc = load_codes(a.pg.k, a.pg.k_scales, off);
+        const Codes vc = load_codes(a.pg.v, a.pg.v_scales, off);
         if (done >= kRing && !wait.warp(Smem::k_empty + st, parity)) return;
-        store_codes(sbase + Smem::k + st * kTileBytes, tid, k);
+        store_codes(sbase + Smem::k + st * kTileBytes, tid, kc);
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(wait.bar(Smem::k_full + st));
+        if (i + 1 < n) kc = load_codes(a.pg.k, a.pg.k_scales, offset_of(ahead, base + Many::kTile, tid));
         if (done >= kRing && !wait.warp(Smem::v_empty + st, parity)) return;
-        store_codes(sbase + Smem::v + st * kTileBytes, tid, v);
+        store_codes(sbase + Smem::v + st * kTileBytes, tid, vc);
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(wait.bar(Smem::v_full + st));
@@ -242,7 +247,13 @@ __device__ __forceinline__ void issue(const Attend& a, Part c, const int64_t* be
 }
 
 // ---- the softmax ------------------------------------------------------------------------------------------------------------
-template <bool kFp4>
+// 32 logits, of which the first `left` count, less the 16 of the first or second half that are gone (two bits).
+__device__ __forceinline__ void hide(uint32_t (&v)[32], int left, uint32_t gone) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j >= left || ((gone >> (j >> 4)) & 1u)) v[j] = 0xff800000u;
+}
+template <bool kFp4, bool kCap>
 __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint8_t* smem, uint32_t sbase,
                                         uint32_t tmem) {
   using E = ManyOf<kFp4>;
@@ -277,7 +288,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
         for (int i = 0; i < 64; ++i) raw[i] = pack(true, __uint_as_float(raw[i] << 16) * down, __uint_as_float(raw[i] & 0xffff0000u) * down);
         f *= __uint_as_float((uint32_t)e << 23) * a.pg.k_scale;
       }
-      if (a.softcap > 0.f) f *= 2.f / a.softcap;
+      if (kCap) f *= 2.f / a.softcap;
 #pragma unroll
       for (int j = 0; j < 16; ++j) sts128(piece(sbase + Smem::q + x * kTileBytes, r, j), w[j]);
       fence_proxy_async();
@@ -293,38 +304,34 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
         ok = wait.warp(Smem::s_full + x, done & 1);
         if (!ok) break;
         tc_fence_after();
-        // twice over the row, 32 columns at a time (the next ones on their way): its maximum, then its weights.  To hold all 128 took
-        // more registers than a softmax warp can have.
+        // twice over the row, 32 columns at a time (the next ones on their way): its maximum, then its weights.  To hold all 128 takes more
+        // registers than a softmax warp can have, and code unrolled further more than the instruction cache has (a fifth of the
+        // stalls).
         const bool masked = base + Many::kTile > c.u.full || gone;
-        uint32_t s[2][32];
-        auto hide = [&](uint32_t (&v)[32], int p) {
-          if (masked) {
-            const int left = (gone >> (2 * p)) & 1u ? 0 : (gone >> (2 * p + 1)) & 1u ? min(lim - base - 32 * p, 16) : lim - base - 32 * p;
-            const bool second = ((gone >> (2 * p)) & 3u) == 1u;           // (the first 16 of the 32 gone, the others there)
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (second ? j < 16 || base + 32 * p + j >= lim : j >= left) v[j] = 0xff800000u;
-          }
-        };
+        const int left = lim - base;
+        uint32_t s0[32], s1[32];
         float t0 = -CUDART_INF_F, t1 = -CUDART_INF_F;
-        tmem_ld32(ts, s[0]);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          tmem_ld_wait_for(s[p & 1]);
-          tmem_ld32(ts + 32 * ((p + 1) & 3), s[(p + 1) & 1]);             // (behind the last: the first again)
-          hide(s[p & 1], p);
+        auto largest = [&](uint32_t (&v)[32], int p) {
+          if (masked) hide(v, left - 32 * p, gone >> (2 * p));
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            t0 = max3(t0, __uint_as_float(s[p & 1][j]), __uint_as_float(s[p & 1][j + 1]));
-            t1 = max3(t1, __uint_as_float(s[p & 1][j + 2]), __uint_as_float(s[p & 1][j + 3]));
+            t0 = max3(t0, __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
+            t1 = max3(t1, __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
           }
+        };
+        tmem_ld32(ts, s0);
+#pragma unroll 1
+        for (int p = 0; p < 4; p += 2) {
+          tmem_ld_wait_for(s0);
+          tmem_ld32(ts + 32 * (p + 1), s1);
+          largest(s0, p);
+          tmem_ld_wait_for(s1);
+          tmem_ld32(ts + 32 * ((p + 2) & 3), s0);                         // (behind the last: the first again)
+          largest(s1, p + 1);
         }
-        tmem_ld_wait_for(s[0]);
-        float top = fmaxf(t0, t1) * f, g = f;
-        if (a.softcap > 0.f) {
-          top = top == -CUDART_INF_F ? top : capped(top, a.softcap * 1.44269504f);      // (the cap keeps the order)
-          g = 1.f;
-        }
+        float top = fmaxf(t0, t1) * f;
+        if (kCap) top = top == -CUDART_INF_F ? top : capped(top, a.softcap * 1.44269504f);      // (the cap keeps the order)
+        tmem_ld_wait_for(s0);
         if (__any_sync(0xffffffffu, top > m + kSlack)) {
           const float now = fmaxf(m, top), alpha = ex2(m - now);
           m = now;
@@ -345,18 +352,14 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
             tmem_st_wait();
           }
         }
-        const float2 g2 = make_float2(g, g), off = make_float2(E::kLift - m, E::kLift - m);
+        const float2 g2 = kCap ? make_float2(1.f, 1.f) : make_float2(f, f), off = make_float2(E::kLift - m, E::kLift - m);
         float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          uint32_t (&v)[32] = s[p & 1];
-          if (p > 0) tmem_ld_wait_for(v);
-          if (p < 3) tmem_ld32(ts + 32 * (p + 1), s[(p + 1) & 1]);
-          if (a.softcap > 0.f) {
+        auto weigh = [&](uint32_t (&v)[32], int p) {
+          if (kCap) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(capped(__uint_as_float(v[j]) * f, a.softcap * 1.44269504f));
           }
-          hide(v, p);
+          if (masked) hide(v, left - 32 * p, gone >> (2 * p));
           uint32_t pk[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -365,6 +368,15 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
             pk[j] = pack(kFp4, w.x, w.y);
           }
           tmem_st16(ts + 16 * p, pk);                                     // (columns that have been read)
+        };
+#pragma unroll 1
+        for (int p = 0; p < 4; p += 2) {
+          if (p > 0) tmem_ld_wait_for(s0);
+          tmem_ld32(ts + 32 * (p + 1), s1);
+          weigh(s0, p);
+          tmem_ld_wait_for(s1);
+          if (p < 2) tmem_ld32(ts + 32 * (p + 2), s0);
+          weigh(s1, p + 1);
         }
         l += sum.x + sum.y;
         tmem_st_wait();
@@ -424,7 +436,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
   }
 }
 
-template <bool kFp4>
+template <bool kFp4, bool kCap>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_attend_many_kernel(const __grid_constant__ Attend a) {
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -460,7 +472,7 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
   Part c;
   if (take_run<Many>(a, before, run, c)) {
     if (warp < 8) {
-      softmax<kFp4>(a, c, before, run, wait, smem, sbase, tmem);
+      softmax<kFp4, kCap>(a, c, before, run, wait, smem, sbase, tmem);
     } else if (warp < 12) {
       produce<kFp4>(a, c, before, run, wait, sbase);
     } else {
@@ -475,11 +487,11 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
   }
 }
 
-template <bool kFp4>
+template <bool kFp4, bool kCap>
 cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
-  cudaError_t e = cudaFuncSetAttribute(paged_attend_many_kernel<kFp4>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::total);
+  cudaError_t e = cudaFuncSetAttribute(paged_attend_many_kernel<kFp4, kCap>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::total);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_attend_many_kernel<kFp4>, dim3((unsigned)most_ctas<Many>(a, n_sm)), dim3(kThreads), Smem::total, s, 1, a);
+  return launch_pdl(paged_attend_many_kernel<kFp4, kCap>, dim3((unsigned)most_ctas<Many>(a, n_sm)), dim3(kThreads), Smem::total, s, 1, a);
 }
 
 }  // namespace
@@ -489,7 +501,8 @@ size_t attend_many_part_floats() { return 2 * (size_t)kSlotFloats<Many>; }
 cudaError_t launch_attend_many(const Attend& in, int n_sm, cudaStream_t s) {
   Attend a = in;
   if (a.wait_limit <= 0) a.wait_limit = ptx::kWaitLimit;
-  return a.pg.fp4 ? go<true>(a, n_sm, s) : go<false>(a, n_sm, s);
+  if (a.softcap > 0.f) return a.pg.fp4 ? go<true, true>(a, n_sm, s) : go<false, true>(a, n_sm, s);
+  return a.pg.fp4 ? go<true, false>(a, n_sm, s) : go<false, false>(a, n_sm, s);
 }
 
 }  // namespace dapq

@@ -304,34 +304,33 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
         ok = wait.warp(Smem::s_full + x, done & 1);
         if (!ok) break;
         tc_fence_after();
-        // twice over the row, 32 columns at a time (the next ones on their way): its maximum, then its weights.  To hold all 128 takes more
-        // registers than a softmax warp can have, and code unrolled further more than the instruction cache has (a fifth of the
-        // stalls).
-        const bool masked = base + Many::kTile > c.u.full || gone;
-        const int left = lim - base;
-        uint32_t s0[32], s1[32];
-        float t0 = -CUDART_INF_F, t1 = -CUDART_INF_F;
-        auto largest = [&](uint32_t (&v)[32], int p) {
-          if (masked) hide(v, left - 32 * p, gone >> (2 * p));
+        uint32_t s[128];
 #pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            t0 = max3(t0, __uint_as_float(v[j]), __uint_as_float(v[j + 1]));
-            t1 = max3(t1, __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
-          }
-        };
-        tmem_ld32(ts, s0);
-#pragma unroll 1
-        for (int p = 0; p < 4; p += 2) {
-          tmem_ld_wait_for(s0);
-          tmem_ld32(ts + 32 * (p + 1), s1);
-          largest(s0, p);
-          tmem_ld_wait_for(s1);
-          tmem_ld32(ts + 32 * ((p + 2) & 3), s0);                         // (behind the last: the first again)
-          largest(s1, p + 1);
+        for (int p = 0; p < 4; ++p) tmem_ld32(ts + 32 * p, s + 32 * p);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) tmem_ld_wait_for(s + 32 * p);
+        if (kCap) {
+#pragma unroll
+          for (int j = 0; j < 128; ++j) s[j] = __float_as_uint(capped(__uint_as_float(s[j]) * f, a.softcap * 1.44269504f));
         }
-        float top = fmaxf(t0, t1) * f;
-        if (kCap) top = top == -CUDART_INF_F ? top : capped(top, a.softcap * 1.44269504f);      // (the cap keeps the order)
-        tmem_ld_wait_for(s0);
+        if (base + Many::kTile > c.u.full || gone) {
+          const int left = lim - base;
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if (j >= left || ((gone >> (j >> 4)) & 1u)) s[j] = 0xff800000u;
+        }
+        const float g = kCap ? 1.f : f;
+        float t0 = __uint_as_float(s[0]), t1 = __uint_as_float(s[1]), t2 = __uint_as_float(s[2]), t3 = __uint_as_float(s[3]);
+#pragma unroll
+        for (int j = 4; j < 124; j += 8) {
+          t0 = max3(t0, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+          t1 = max3(t1, __uint_as_float(s[j + 2]), __uint_as_float(s[j + 3]));
+          t2 = max3(t2, __uint_as_float(s[j + 4]), __uint_as_float(s[j + 5]));
+          t3 = max3(t3, __uint_as_float(s[j + 6]), __uint_as_float(s[j + 7]));
+        }
+        t0 = max3(t0, __uint_as_float(s[124]), __uint_as_float(s[125]));
+        t1 = max3(t1, __uint_as_float(s[126]), __uint_as_float(s[127]));
+        const float top = fmaxf(max3(t0, t1, t2), t3) * g;
         if (__any_sync(0xffffffffu, top > m + kSlack)) {
           const float now = fmaxf(m, top), alpha = ex2(m - now);
           m = now;
@@ -352,31 +351,19 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
             tmem_st_wait();
           }
         }
-        const float2 g2 = kCap ? make_float2(1.f, 1.f) : make_float2(f, f), off = make_float2(E::kLift - m, E::kLift - m);
+        const float2 g2 = make_float2(g, g), off = make_float2(E::kLift - m, E::kLift - m);
         float2 sum = make_float2(0.f, 0.f);
-        auto weigh = [&](uint32_t (&v)[32], int p) {
-          if (kCap) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(capped(__uint_as_float(v[j]) * f, a.softcap * 1.44269504f));
-          }
-          if (masked) hide(v, left - 32 * p, gone >> (2 * p));
-          uint32_t pk[16];
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t pk[32];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float2 w = ex2_pair_mufu(__ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), g2, off));
+          for (int j = 0; j < 32; ++j) {
+            const int at = 64 * hf + 2 * j;
+            const float2 w = ex2_pair_mufu(__ffma2_rn(make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), g2, off));
             sum = __fadd2_rn(sum, w);
             pk[j] = pack(kFp4, w.x, w.y);
           }
-          tmem_st16(ts + 16 * p, pk);                                     // (columns that have been read)
-        };
-#pragma unroll 1
-        for (int p = 0; p < 4; p += 2) {
-          if (p > 0) tmem_ld_wait_for(s0);
-          tmem_ld32(ts + 32 * (p + 1), s1);
-          weigh(s0, p);
-          tmem_ld_wait_for(s1);
-          if (p < 2) tmem_ld32(ts + 32 * (p + 2), s0);
-          weigh(s1, p + 1);
+          tmem_st32(ts + 32 * hf, pk);
         }
         l += sum.x + sum.y;
         tmem_st_wait();
@@ -471,11 +458,15 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
   Run run;
   Part c;
   if (take_run<Many>(a, before, run, c)) {
+    // registers: 256 x 184 + 128 x 88 + 128 x 56, the 65536 that the block was launched with
     if (warp < 8) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
       softmax<kFp4, kCap>(a, c, before, run, wait, smem, sbase, tmem);
     } else if (warp < 12) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
       produce<kFp4>(a, c, before, run, wait, sbase);
     } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
       if (warp == 12 && lane == 0) issue<kFp4>(a, c, before, run, wait, sbase, tmem);
     }
   }

@@ -192,46 +192,63 @@ __device__ __forceinline__ void produce(const Attend& a, Part c, const int64_t* 
 }
 
 // ---- the MMAs ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0u;
+}
+// A whole warp walks the tiles, one of its lanes issues: what the instructions take is then uniform, and stays in uniform registers.  (With the
+// walk in one lane's branch every operand was moved there for every MMA, and issuing, not the products, set the pace: 120 cycles each.)
 template <bool kFp4>
 __device__ __forceinline__ void issue(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint32_t sbase, uint32_t tmem) {
-  const uint32_t idesc_s = kFp4 ? umma_idesc_f16(128, 128) : umma_idesc(128, 128), idesc_o = idesc_s | (1u << 16);   // (V: MN-major)
-  int done = 0, parts = 0, parts_b = 0, done_b = 0;
+  constexpr uint32_t idesc_s = kFp4 ? umma_idesc_f16(128, 128) : umma_idesc(128, 128), idesc_o = idesc_s | (1u << 16);   // (V: MN-major)
+  uint32_t done = 0, parts = 0, parts_b = 0, done_b = 0;
   bool ok = true;
-  auto scores = [&](int x, int st) {                                      // S of tile x
-    const uint64_t q = umma_desc(sbase + Smem::q + x * kTileBytes), k = umma_desc(sbase + Smem::k + st * kTileBytes);
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
-      umma_ss(tmem + x * 128, desc_advance(q, (ks >> 2) * kHalfTile + (ks & 3) * 32), desc_advance(k, (ks >> 2) * kHalfTile + (ks & 3) * 32), idesc_s, ks ? 1u : 0u);
-    tc_commit(wait.bar(Smem::s_full + x));
+  auto commit = [&](int i) {
+    if (elect_one()) tc_commit(wait.bar(i));
   };
-  auto outputs = [&](int x, int st, bool more) {                          // O of tile x
-    const uint64_t v = values_desc(sbase + Smem::v + st * kTileBytes);
+  auto scores = [&](uint32_t x, uint32_t st) {                            // S of tile x
+    const uint64_t q = umma_desc(sbase + Smem::q + x * kTileBytes), k = umma_desc(sbase + Smem::k + st * kTileBytes);
+    if (elect_one()) {
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) umma_ts(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, desc_advance(v, ks * 2048), idesc_o, more || ks ? 1u : 0u);
-    tc_commit(wait.bar(Smem::pv_done + x));
+      for (int ks = 0; ks < 8; ++ks)
+        umma_ss(tmem + x * 128, desc_advance(q, (ks >> 2) * kHalfTile + (ks & 3) * 32), desc_advance(k, (ks >> 2) * kHalfTile + (ks & 3) * 32), idesc_s, ks ? 1u : 0u);
+      tc_commit(wait.bar(Smem::s_full + x));
+    }
+    __syncwarp();
+  };
+  auto outputs = [&](uint32_t x, uint32_t st, bool more) {                // O of tile x
+    const uint64_t v = values_desc(sbase + Smem::v + st * kTileBytes);
+    if (elect_one()) {
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) umma_ts(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, desc_advance(v, ks * 2048), idesc_o, more || ks ? 1u : 0u);
+      tc_commit(wait.bar(Smem::pv_done + x));
+    }
+    __syncwarp();
   };
   for (bool on = true; on && ok; on = next<Many>(a, c, before, run.end)) {
-    const int n = (int)(c.end - c.begin);
-    const bool two = c.u.rows - c.u.row0 > 128;
-    ok = wait(Smem::q_full, parts & 1) && (!two || wait(Smem::q_full + 1, parts_b & 1)) && wait(Smem::k_full + (done & 1), (done >> 1) & 1);
+    const int n = __shfl_sync(0xffffffffu, (int)(c.end - c.begin), 0);
+    const bool two = __shfl_sync(0xffffffffu, c.u.rows - c.u.row0, 0) > 128;
+    ok = wait.warp(Smem::q_full, parts & 1) && (!two || wait.warp(Smem::q_full + 1, parts_b & 1)) && wait.warp(Smem::k_full + (done & 1), (done >> 1) & 1);
     if (!ok) break;
     tc_fence_after();
     scores(0, done & 1);
     if (two) scores(1, done & 1);
-    tc_commit(wait.bar(Smem::k_empty + (done & 1)));
+    commit(Smem::k_empty + (done & 1));
     for (int i = 0; i < n && ok; ++i) {
-      const int t = done + i, st = t & 1, st1 = st ^ 1;
-      ok = wait(Smem::v_full + st, (t >> 1) & 1);
-      if (ok && i + 1 < n) ok = wait(Smem::k_full + st1, ((t + 1) >> 1) & 1);
-      for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-        ok = wait(Smem::p_full + x, (x ? done_b + i : t) & 1);
+      const uint32_t t = done + i, st = t & 1, st1 = st ^ 1;
+      ok = wait.warp(Smem::v_full + st, (t >> 1) & 1);
+      if (ok && i + 1 < n) ok = wait.warp(Smem::k_full + st1, ((t + 1) >> 1) & 1);
+#pragma unroll 1
+      for (uint32_t x = 0; x < (two ? 2u : 1u) && ok; ++x) {
+        ok = wait.warp(Smem::p_full + x, (x ? done_b + i : t) & 1);
         if (!ok) break;
         tc_fence_after();
         outputs(x, st, i > 0);
         if (i + 1 < n) scores(x, st1);
       }
-      tc_commit(wait.bar(Smem::v_empty + st));
-      if (i + 1 < n) tc_commit(wait.bar(Smem::k_empty + st1));
+      commit(Smem::v_empty + st);
+      if (i + 1 < n) commit(Smem::k_empty + st1);
     }
     done += n;
     ++parts;
@@ -241,7 +258,7 @@ __device__ __forceinline__ void issue(const Attend& a, Part c, const int64_t* be
     }
   }
   if (!ok) {                                                              // see what was issued retire before tensor memory goes
-    tc_commit(wait.bar(Smem::drain));
+    commit(Smem::drain);
     drain_wait(wait.bar(Smem::drain), 0, kWaitLimit);
   }
 }
@@ -252,6 +269,45 @@ __device__ __forceinline__ void hide(uint32_t (&v)[32], int left, uint32_t gone)
 #pragma unroll
   for (int j = 0; j < 32; ++j)
     if (j >= left || ((gone >> (j >> 4)) & 1u)) v[j] = 0xff800000u;
+}
+// The rows of a unit from the partial results of the CTAs that share it, in their order: a warp takes rows warp, warp + 8, .., and of these
+// kAtOnce together, whose loads are in flight together (one after the other they took a seventh of the kernel's time).
+template <class E>
+__device__ __forceinline__ void merge_rows(const Attend& a, const Unit& u, const Share<E>& share, int warp, int lane) {
+  constexpr int kAtOnce = 8;
+#pragma unroll 1
+  for (int y0 = warp; y0 < Many::kRows && u.row0 + y0 < u.rows; y0 += 8 * kAtOnce) {
+    float4 acc[kAtOnce];
+    float top[kAtOnce], sum[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      top[k] = kLowest;
+      sum[k] = 0.f;
+    }
+#pragma unroll 1
+    for (int x = 0; x < share.n; ++x) {
+      const float* from = x == 0 ? share.first : share.others + 2 * (int64_t)x * kSlotFloats<E>;
+      float4 v[kAtOnce];
+      float2 st[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int y = min(y0 + 8 * k, Many::kRows - 1);
+        v[k] = __ldcg(reinterpret_cast<const float4*>(from + y * kHeadDim) + lane);
+        st[k] = __ldcg(reinterpret_cast<const float2*>(from + E::kSlotRows * kHeadDim) + y);
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float now = fmaxf(top[k], st[k].x), f = ex2(top[k] - now), g = ex2(st[k].x - now);
+        top[k] = now;
+        sum[k] = fmaf(sum[k], f, g * st[k].y);
+        acc[k] = make_float4(fmaf(acc[k].x, f, g * v[k].x), fmaf(acc[k].y, f, g * v[k].y), fmaf(acc[k].z, f, g * v[k].z), fmaf(acc[k].w, f, g * v[k].w));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (y0 + 8 * k < Many::kRows) write_row<E>(a, u, y0 + 8 * k, acc[k], top[k], sum[k], lane);
+  }
 }
 template <bool kFp4, bool kCap>
 __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint8_t* smem, uint32_t sbase,
@@ -415,7 +471,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
       softmax_sync();
       if (*last_here) {
         __threadfence();
-        for (int y = warp; y < Many::kRows && c.u.row0 + y < c.u.rows; y += 8) merge_row<E>(a, c.u, y, share.first, share.others, share.n, lane);
+        merge_rows<E>(a, c.u, share, warp, lane);
         if (threadIdx.x == 0) a.sync[share.c0] = 0u;
       }
       softmax_sync();
@@ -467,7 +523,7 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
       produce<kFp4>(a, c, before, run, wait, sbase);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-      if (warp == 12 && lane == 0) issue<kFp4>(a, c, before, run, wait, sbase, tmem);
+      if (warp == 12) issue<kFp4>(a, c, before, run, wait, sbase, tmem);
     }
   }
   tc_fence_before();

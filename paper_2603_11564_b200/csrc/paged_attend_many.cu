@@ -25,7 +25,7 @@ constexpr int kRing = 2;                              // tiles of K, and of V, i
 struct Smem {
   static constexpr int q = 0, k = 2 * kTileBytes, v = k + kRing * kTileBytes, bars = v + kRing * kTileBytes;
   // barriers
-  static constexpr int k_full = 0, k_empty = 2, v_full = 4, v_empty = 6, q_full = 8, s_full = 10, p_full = 12, pv_done = 14, drain = 16, n_bars = 17;
+  static constexpr int k_full = 0, k_empty = 2, v_full = 4, v_empty = 6, q_full = 8, s_full = 10, p_half = 12, p_full = 14, pv_done = 16, drain = 18, n_bars = 19;
   static constexpr int before = bars + 8 * n_bars, tmem_ptr = before + 8 * (kMaxBatch + 1), abort_flag = tmem_ptr + 4, last_here = abort_flag + 4,
                        total = last_here + 4;
 };
@@ -125,67 +125,86 @@ __device__ __forceinline__ void store_codes(uint32_t tile, int r, const Codes& c
   }
 }
 
+// Keys go one tile ahead of the values: tile t's second product and tile t + 1's first follow one another.
 template <bool kFp4>
 __device__ __forceinline__ void produce(const Attend& a, Part c, const int64_t* before, const Run& run, const Wait& wait, uint32_t sbase) {
   const int tid = threadIdx.x - 256, lane = tid & 31, warp = tid >> 5;
   int done = 0;                                                           // tiles so far
-  Codes kc;
   for (bool on = true; on; on = next<Many>(a, c, before, run.end)) {
     const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile;
-    int page = tile_page(a, c.u, first, lane), ahead = 0;
-    auto offset_of = [&](int pages, int base, int r) {                    // channel offset of row r of a tile, negative: reads as zero
+    auto offset = [&](int pages, int base, int r) {                       // channel offset of row r of a tile, negative: reads as zero
       const int pg = __shfl_sync(0xffffffffu, pages, r >> 4);
       return (unsigned)pg >= (unsigned)a.pg.n_pages || base + r >= c.u.limit
                  ? (int64_t)-1
                  : pg * a.pg.page_stride + c.u.h * a.pg.head_stride + (int64_t)((base + r) & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride;
     };
-    for (int i = 0; i < n; ++i, ++done, page = ahead) {
-      const int base = first + i * Many::kTile, st = done & 1;
-      const bool sound = (unsigned)page < (unsigned)a.pg.n_pages;
-      if (warp == 0 && lane < 8 && base + 16 * lane < c.u.limit && !sound) atomicOr(a.status, kStatusBadPage);
-      if (i + 1 < n) ahead = tile_page(a, c.u, base + Many::kTile, lane);
-      auto offset = [&](int r) { return offset_of(page, base, r); };
-      const uint32_t parity = ((done >> 1) & 1) ^ 1;
-      if constexpr (kFp4) {
-        // (a row's codes are on their way while those before them are turned into operands)
-        const int64_t off = offset(tid);
-        if (i == 0) kc = load_codes(a.pg.k, a.pg.k_scales, off);
-        const Codes vc = load_codes(a.pg.v, a.pg.v_scales, off);
-        if (done >= kRing && !wait.warp(Smem::k_empty + st, parity)) return;
-        store_codes(sbase + Smem::k + st * kTileBytes, tid, kc);
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(wait.bar(Smem::k_full + st));
-        if (i + 1 < n) kc = load_codes(a.pg.k, a.pg.k_scales, offset_of(ahead, base + Many::kTile, tid));
-        if (done >= kRing && !wait.warp(Smem::v_empty + st, parity)) return;
-        store_codes(sbase + Smem::v + st * kTileBytes, tid, vc);
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(wait.bar(Smem::v_full + st));
-      } else {
-        auto copy = [&](uint32_t tile, const char* from) {
+    auto check = [&](int pages, int base) {
+      if (warp == 0 && lane < 8 && base + 16 * lane < c.u.limit && (unsigned)pages >= (unsigned)a.pg.n_pages) atomicOr(a.status, kStatusBadPage);
+    };
+    auto free = [&](int which, int t) { return t < kRing || wait.warp(which + (t & 1), ((t >> 1) & 1) ^ 1); };
+    auto full = [&](int which, int t) {
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(wait.bar(which + (t & 1)));
+    };
+    int page = tile_page(a, c.u, first, lane), page1 = n > 1 ? tile_page(a, c.u, first + Many::kTile, lane) : -1;
+    check(page, first);
+    if constexpr (kFp4) {
+      // (a row's codes are on their way while those before them are turned into operands)
+      Codes k = load_codes(a.pg.k, a.pg.k_scales, offset(page, first, tid));
+      if (!free(Smem::k_empty, done)) return;
+      store_codes(sbase + Smem::k + (done & 1) * kTileBytes, tid, k);
+      full(Smem::k_full, done);
+      if (n > 1) k = load_codes(a.pg.k, a.pg.k_scales, offset(page1, first + Many::kTile, tid));
+      for (int i = 0; i < n; ++i, ++done) {
+        const int base = first + i * Many::kTile;
+        const Codes v = load_codes(a.pg.v, a.pg.v_scales, offset(page, base, tid));
+        const int page2 = i + 2 < n ? tile_page(a, c.u, base + 2 * Many::kTile, lane) : -1;
+        if (i + 1 < n) {
+          check(page1, base + Many::kTile);
+          if (!free(Smem::k_empty, done + 1)) return;
+          store_codes(sbase + Smem::k + ((done + 1) & 1) * kTileBytes, tid, k);
+          full(Smem::k_full, done + 1);
+        }
+        if (i + 2 < n) k = load_codes(a.pg.k, a.pg.k_scales, offset(page2, base + 2 * Many::kTile, tid));
+        if (!free(Smem::v_empty, done)) return;
+        store_codes(sbase + Smem::v + (done & 1) * kTileBytes, tid, v);
+        full(Smem::v_full, done);
+        page = page1;
+        page1 = page2;
+      }
+    } else {
+      auto copy = [&](uint32_t tile, const char* from, int pages, int base) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int r = 8 * j + (tid >> 4);
-            const int64_t off = offset(r);
-            const uint32_t to = piece(tile, r, tid & 15);
-            if (off < 0) sts128(to, make_uint4(0, 0, 0, 0));
-            else cp_async16(to, from + 2 * off + (tid & 15) * 16);
-          }
-          cp_async_commit();
-        };
-        if (done >= kRing && !wait.warp(Smem::k_empty + st, parity)) { cp_async_wait<0>(); return; }
-        copy(sbase + Smem::k + st * kTileBytes, a.pg.k);
-        if (done >= kRing && !wait.warp(Smem::v_empty + st, parity)) { cp_async_wait<0>(); return; }
-        copy(sbase + Smem::v + st * kTileBytes, a.pg.v);
+        for (int j = 0; j < 16; ++j) {
+          const int r = 8 * j + (tid >> 4);
+          const int64_t off = offset(pages, base, r);
+          const uint32_t to = piece(tile, r, tid & 15);
+          if (off < 0) sts128(to, make_uint4(0, 0, 0, 0));
+          else cp_async16(to, from + 2 * off + (tid & 15) * 16);
+        }
+        cp_async_commit();
+      };
+      if (!free(Smem::k_empty, done)) return;
+      copy(sbase + Smem::k + (done & 1) * kTileBytes, a.pg.k, page, first);
+      cp_async_wait<0>();
+      full(Smem::k_full, done);
+      for (int i = 0; i < n; ++i, ++done) {
+        const int base = first + i * Many::kTile;
+        const int page2 = i + 2 < n ? tile_page(a, c.u, base + 2 * Many::kTile, lane) : -1;
+        if (i + 1 < n) {
+          check(page1, base + Many::kTile);
+          if (!free(Smem::k_empty, done + 1)) return;
+          copy(sbase + Smem::k + ((done + 1) & 1) * kTileBytes, a.pg.k, page1, base + Many::kTile);
+        }
+        if (!free(Smem::v_empty, done)) { cp_async_wait<0>(); return; }
+        copy(sbase + Smem::v + (done & 1) * kTileBytes, a.pg.v, page, base);
         cp_async_wait<1>();
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(wait.bar(Smem::k_full + st));
+        if (i + 1 < n) full(Smem::k_full, done + 1);
         cp_async_wait<0>();
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(wait.bar(Smem::v_full + st));
+        full(Smem::v_full, done);
+        page = page1;
+        page1 = page2;
       }
     }
   }
@@ -217,12 +236,13 @@ __device__ __forceinline__ void issue(const Attend& a, Part c, const int64_t* be
     }
     __syncwarp();
   };
-  auto outputs = [&](uint32_t x, uint32_t st, bool more) {                // O of tile x
+  auto outputs = [&](uint32_t x, uint32_t st, int k0, bool more) {        // O of tile x over 64 keys
     const uint64_t v = values_desc(sbase + Smem::v + st * kTileBytes);
     if (elect_one()) {
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks) umma_ts(tmem + 256 + x * 128, tmem + x * 128 + ks * 8, desc_advance(v, ks * 2048), idesc_o, more || ks ? 1u : 0u);
-      tc_commit(wait.bar(Smem::pv_done + x));
+      for (int ks = 0; ks < 4; ++ks)
+        umma_ts(tmem + 256 + x * 128, tmem + x * 128 + (k0 + ks) * 8, desc_advance(v, (k0 + ks) * 2048), idesc_o, more || ks ? 1u : 0u);
+      if (k0) tc_commit(wait.bar(Smem::pv_done + x));
     }
     __syncwarp();
   };
@@ -241,10 +261,15 @@ __device__ __forceinline__ void issue(const Attend& a, Part c, const int64_t* be
       if (ok && i + 1 < n) ok = wait.warp(Smem::k_full + st1, ((t + 1) >> 1) & 1);
 #pragma unroll 1
       for (uint32_t x = 0; x < (two ? 2u : 1u) && ok; ++x) {
-        ok = wait.warp(Smem::p_full + x, (x ? done_b + i : t) & 1);
+        const uint32_t parity = (x ? done_b + i : t) & 1;
+        ok = wait.warp(Smem::p_half + x, parity);
         if (!ok) break;
         tc_fence_after();
-        outputs(x, st, i > 0);
+        outputs(x, st, 0, i > 0);
+        ok = wait.warp(Smem::p_full + x, parity);
+        if (!ok) break;
+        tc_fence_after();
+        outputs(x, st, 4, true);
         if (i + 1 < n) scores(x, st1);
       }
       commit(Smem::v_empty + st);
@@ -410,22 +435,24 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const int64_t* 
         const float2 g2 = make_float2(g, g), off = make_float2(E::kLift - m, E::kLift - m);
         float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t pk[32];
+        for (int p = 0; p < 4; ++p) {
+          uint32_t pk[16];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const int at = 64 * hf + 2 * j;
+          for (int j = 0; j < 16; ++j) {
+            const int at = 32 * p + 2 * j;
             const float2 w = ex2_pair_mufu(__ffma2_rn(make_float2(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), g2, off));
             sum = __fadd2_rn(sum, w);
             pk[j] = pack(kFp4, w.x, w.y);
           }
-          tmem_st32(ts + 32 * hf, pk);
+          tmem_st16(ts + 16 * p, pk);
+          if (p & 1) {                                                    // (the product over the first 64 keys can begin)
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(wait.bar((p == 1 ? Smem::p_half : Smem::p_full) + x));
+          }
         }
         l += sum.x + sum.y;
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(wait.bar(Smem::p_full + x));
       }
       if (ok) ok = wait.warp(Smem::pv_done + x, (done - 1) & 1);
       if (ok) {
@@ -494,7 +521,7 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
   if (threadIdx.x == 0) {
     for (int i = 0; i < Smem::n_bars; ++i) {
       const bool four = i < Smem::k_empty || i == Smem::v_full || i == Smem::v_full + 1 || (i >= Smem::q_full && i < Smem::s_full) ||
-                        (i >= Smem::p_full && i < Smem::pv_done);
+                        (i >= Smem::p_half && i < Smem::pv_done);
       mbar_init(wait.bar(i), four ? 4 : 1);                               // the warps of a role, or the issuer's commit
     }
     *wait.abort_flag = 0;

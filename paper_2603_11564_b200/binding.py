@@ -88,6 +88,7 @@ class dapq_paged_cache(C.Structure):
                          table_stride=page_table.shape[1], n_pages=k.shape[0], page_rows=k.shape[2],
                          format=DAPQ_CACHE_FP4 if fp4 else DAPQ_CACHE_NATIVE, k_scale=k_scale, v_scale=v_scale, batch=page_table.shape[0])
         self.tensors = (k, v, page_table, cache_len, k_scales, v_scales)
+        self.address = C.addressof(self)            # (what the calls pass: ctypes takes half a microsecond to find it)
 
 
 class dapq_new_tokens(C.Structure):
@@ -145,7 +146,7 @@ def load_library() -> C.CDLL:
     lib.dapq_evict_host.restype = C.c_int
     lib.dapq_recall.argtypes = [vp, vp, vp, i32p, i32p, C.c_int32, f32p, vp]
     lib.dapq_recall.restype = C.c_int
-    pages = C.POINTER(dapq_paged_cache)
+    pages = C.c_void_p
     lib.dapq_paged_append.argtypes = [vp, pages, i32p, C.c_void_p, vp]
     lib.dapq_paged_append.restype = C.c_int
     lib.dapq_paged_compact.argtypes = [vp, view, vp, i32p, pages, vp]
@@ -364,48 +365,66 @@ def dapq_evict_host(ctx, q_pre: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
 _TOKENS = struct.Struct("@PPPPqqqP")                # dapq_new_tokens, field by field
 assert _TOKENS.size == C.sizeof(dapq_new_tokens)
 
+_INT32S: dict = {}                                  # struct.Struct of n int32, by n
+
+
+def _i32_bytes(seq: Optional[Sequence[int]]) -> Optional[bytes]:
+    """int32 image of `seq`.  (The calls of a decode step take a few microseconds on the GPU; packing the offsets of 64 sequences
+    into an array takes one of them, into bytes half of one.)"""
+    if seq is None:
+        return None
+    if type(seq) in (list, tuple):
+        n = len(seq)
+        fmt = _INT32S.get(n)
+        if fmt is None:
+            fmt = _INT32S[n] = struct.Struct("@%di" % n)
+        try:
+            return fmt.pack(*seq)
+        except struct.error:
+            pass                                    # what only numpy converts (or refuses)
+    return np.ascontiguousarray(np.asarray(seq, dtype=np.int32)).tobytes()
+
 
 def _token_stride(x: torch.Tensor) -> int:
     """Elements between the tokens of [T, H, 128]: heads and channels contiguous."""
-    assert x.dim() == 3 and x.shape[2] == 128 and x.stride(2) == 1 and (x.stride(1) == 128 or x.shape[1] == 1)
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * 128
+    s, n = x.stride(), x.shape
+    assert len(s) == 3 and n[2] == 128 and s[2] == 1 and (s[1] == 128 or n[1] == 1)
+    return s[0] if n[0] > 1 else n[1] * 128
 
 
 def dapq_paged_append(ctx, pages: dapq_paged_cache, cu_new, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
                       q: Optional[torch.Tensor] = None, q_rot: Optional[torch.Tensor] = None, stream=None) -> None:
     """cu_new: [B + 1] offsets of the sequences' new tokens, None: one each.  k, v: [T, H_kv, 128], q: [T, H_q, 128], e.g. slices of a
     fused projection; q_rot: contiguous."""
-    cu, cu_p = _i32(cu_new) if cu_new is not None else (None, None)
-    assert q_rot is None or q_rot.is_contiguous()
-    tokens = _TOKENS.pack(k.data_ptr(), v.data_ptr(), _ptr(q) or 0, _ptr(q_rot) or 0, _token_stride(k), _token_stride(v),
-                          _token_stride(q) if q is not None else 0, _ptr(positions) or 0)
-    _check(ctx, load_library().dapq_paged_append(ctx, pages, cu_p, tokens, _stream(stream)))
+    if q is None:
+        tokens = _TOKENS.pack(k.data_ptr(), v.data_ptr(), 0, _ptr(q_rot) or 0, _token_stride(k), _token_stride(v), 0, _ptr(positions) or 0)
+    else:
+        assert q_rot is None or q_rot.is_contiguous()
+        tokens = _TOKENS.pack(k.data_ptr(), v.data_ptr(), q.data_ptr(), _ptr(q_rot) or 0, _token_stride(k), _token_stride(v), _token_stride(q),
+                              _ptr(positions) or 0)
+    _check(ctx, load_library().dapq_paged_append(ctx, pages.address, _i32_bytes(cu_new), tokens, _stream(stream)))
 
 
 def dapq_paged_compact(ctx, k: torch.Tensor, v: torch.Tensor, cu_rows, prompt_len, idx: torch.Tensor, k_keep, pages: dapq_paged_cache,
                        stream=None) -> None:
     view, keep_alive = _view(k, v, cu_rows, prompt_len)
-    kk, kk_p = _i32(k_keep)
-    _check(ctx, load_library().dapq_paged_compact(ctx, view, idx.data_ptr(), kk_p, pages, _stream(stream)))
+    _check(ctx, load_library().dapq_paged_compact(ctx, view, idx.data_ptr(), _i32_bytes(k_keep), pages.address, _stream(stream)))
 
 
 def dapq_paged_read(ctx, pages: dapq_paged_cache, first, n_rows, row_at, k_out: torch.Tensor, v_out: torch.Tensor, stream=None) -> None:
     """k_out, v_out: [H_kv, R, 128], rows contiguous, heads apart alike."""
-    hs = k_out.stride(0) if k_out.shape[0] > 1 else k_out.shape[1] * 128
-    assert k_out.dim() == 3 and k_out.shape == v_out.shape and k_out.stride() == v_out.stride() and k_out.stride()[1:] == (128, 1)
-    fi, fi_p = _i32(first) if first is not None else (None, None)
-    n, n_p = _i32(n_rows)
-    at, at_p = _i32(row_at)
-    _check(ctx, load_library().dapq_paged_read(ctx, pages, fi_p, n_p, at_p, k_out.data_ptr(), v_out.data_ptr(), hs, _stream(stream)))
+    s, n = k_out.stride(), k_out.shape
+    assert len(s) == 3 and n[2] == 128 and s[1:] == (128, 1) and v_out.stride() == s and v_out.shape == n
+    _check(ctx, load_library().dapq_paged_read(ctx, pages.address, _i32_bytes(first), _i32_bytes(n_rows), _i32_bytes(row_at), k_out.data_ptr(),
+                                               v_out.data_ptr(), s[0] if n[0] > 1 else n[1] * 128, _stream(stream)))
 
 
 def dapq_paged_attend(ctx, pages: dapq_paged_cache, cu_new, q_rot: torch.Tensor, out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
                       softcap: float = 0.0, stream=None) -> None:
     """q_rot, out: [T, H_q, 128]; lse_out: [T, H_q] fp32."""
-    cu, cu_p = _i32(cu_new) if cu_new is not None else (None, None)
     assert out.is_contiguous() and (lse_out is None or lse_out.is_contiguous())
-    _check(ctx, load_library().dapq_paged_attend(ctx, pages, cu_p, q_rot.data_ptr(), _token_stride(q_rot), softcap, out.data_ptr(), _ptr(lse_out),
-                                                 _stream(stream)))
+    _check(ctx, load_library().dapq_paged_attend(ctx, pages.address, _i32_bytes(cu_new), q_rot.data_ptr(), _token_stride(q_rot), softcap,
+                                                 out.data_ptr(), _ptr(lse_out), _stream(stream)))
 
 
 DAPQ_STATIC_SCRATCH_BYTES = 2 * 1024 * 1024

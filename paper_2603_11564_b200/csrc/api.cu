@@ -96,12 +96,13 @@ thread_local char g_create_err[256] = "";
 
 struct DeviceGuard {
   int prev = -1;
-  bool ok = true;
+  bool ok = true, changed = false;
   explicit DeviceGuard(int dev) {
     if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    changed = prev != dev;
+    if (changed && cudaSetDevice(dev) != cudaSuccess) ok = false;
   }
-  ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+  ~DeviceGuard() { if (changed) cudaSetDevice(prev); }
 };
 
 dapq_status fail(dapq_ctx* ctx, dapq_status st, const char* fmt, ...) {

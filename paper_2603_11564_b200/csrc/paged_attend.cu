@@ -21,6 +21,7 @@ namespace dapq {
 namespace {
 
 constexpr int kPadRow = 132;                         // floats of a row of the warps' partial outputs (conflict-free, see flush)
+__device__ __forceinline__ float2& row_stats(float* buf, int r) { return *reinterpret_cast<float2*>(buf + r * kPadRow + kHeadDim); }   // its maximum and sum
 
 // ---- pieces ---------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
@@ -77,8 +78,8 @@ __device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t
 template <bool kFp4, int kTiles>
 struct TensorEngine {
   static constexpr int kNT = kTiles;
-  static constexpr int kWarps = 8, kSub = kFp4 && kNT == 1 ? 2 : 1, kTile = kWarps * kSub * 16, kRows = 8 * kNT, kSlotRows = 16, kCtas = 1, kStages = kFp4 ? 4 : 3;
-  static constexpr int kMinRun = 2, kByteShift = kFp4 ? -1 : 1, kSubBytes = kFp4 ? 16 * 144 : 16 * 512, kStageBytes = kSub * kSubBytes;
+  static constexpr int kWarps = 8, kSub = kFp4 && kNT == 1 ? 2 : 1, kTile = kWarps * kSub * 16, kRows = 8 * kNT, kSlotRows = 16, kMergeBatch = 16, kCtas = 1, kStages = kFp4 ? 4 : 3;
+  static constexpr int kMinRun = 4, kByteShift = kFp4 ? -1 : 1, kSubBytes = kFp4 ? 16 * 144 : 16 * 512, kStageBytes = kSub * kSubBytes;
   static constexpr int kExtra = 0;
   static constexpr float kLift = kFp4 ? 11.f : 0.f;
   using T = __nv_bfloat16;
@@ -264,7 +265,7 @@ struct TensorEngine {
   }
   // Keys base .. base + 16 kSub - 1 of the sequence; whole: all of the unit's queries see all of them; gone: pieces of 16 that do not exist.
   template <bool whole>
-  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char*, int, int lane, uint32_t gone = 0u) {
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, uint32_t gone, unsigned char*, int, int lane) {
     const int rk = key_of(lane >> 2);
     float z[kSub][kNT][4];                                                 // base-2 logits
     bool above = false;
@@ -279,9 +280,22 @@ struct TensorEngine {
           float& x = z[b][nt][e];
           x *= fac[nt][e & 1];
           if (a.softcap > 0.f) x = capped(x, a.softcap * 1.44269504f);
-          if (!whole && (base + 16 * b + rk + (e & 2) * 4 >= lim[nt][e & 1] || ((gone >> b) & 1u))) x = -CUDART_INF_F;
-          above = above || x > m[nt][e & 1] + kSlack;
         }
+    if (!whole) {
+#pragma unroll
+      for (int b = 0; b < kSub; ++b)
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (base + 16 * b + rk + (e & 2) * 4 >= lim[nt][e & 1] || ((gone >> b) & 1u)) z[b][nt][e] = -CUDART_INF_F;
+    }
+#pragma unroll
+    for (int b = 0; b < kSub; ++b)
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) above = above || z[b][nt][e] > m[nt][e & 1] + kSlack;
     if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
@@ -330,8 +344,8 @@ struct TensorEngine {
     }
   }
 
-  // The warp's outputs of rows 8 nt .. 8 nt + 7 to buf [8][kPadRow] at position 16 j + 2 g + e, its maxima and sums to ml [8].
-  __device__ __forceinline__ void flush(float* buf, float2* ml, int nt, int lane) const {
+  // The warp's outputs of rows 8 nt .. 8 nt + 7 to buf [8][kPadRow] at position 16 j + 2 g + e, with their maxima and sums.
+  __device__ __forceinline__ void flush(float* buf, int nt, int lane) const {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
@@ -341,7 +355,7 @@ struct TensorEngine {
         float sum = l[n][e];
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-        if (g == 0) ml[2 * t + e] = make_float2(m[n][e], sum);
+        if (g == 0) row_stats(buf, 2 * t + e) = make_float2(m[n][e], sum);
 #pragma unroll
         for (int j = 0; j < 8; ++j) *reinterpret_cast<float2*>(buf + (2 * t + e) * kPadRow + 16 * j + 2 * g) = make_float2(o[n][j][e], o[n][j][e + 2]);
       }
@@ -359,7 +373,7 @@ struct TensorEngine {
 // outputs, queries and weights broadcast from shared memory.
 template <bool kFp4>
 struct FloatEngine {
-  static constexpr int kWarps = 4, kSub = 1, kTile = kWarps * 16, kRows = 8, kSlotRows = 16, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
+  static constexpr int kWarps = 4, kSub = 1, kTile = kWarps * 16, kRows = 8, kSlotRows = 16, kMergeBatch = 16, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
   static constexpr int kSubBytes = kFp4 ? 16 * 144 : 16 * 1024, kStageBytes = kSubBytes;
   static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = 16 * kRows * 4;
   static constexpr int kExtra = kQBytes + kWarps * kPBytes;
@@ -413,7 +427,7 @@ struct FloatEngine {
   }
 
   template <bool whole>
-  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, unsigned char* extra, int warp, int lane, uint32_t gone = 0u) {
+  __device__ __forceinline__ void step(const Attend& a, const Unit& u, uint32_t stage, int base, uint32_t gone, unsigned char* extra, int warp, int lane) {
     if (!whole && gone) return;
     const int key = lane >> 1, hf = lane & 1;
     const uint32_t qs = smem_u32(extra), ps = qs + kQBytes + warp * kPBytes;
@@ -511,13 +525,13 @@ struct FloatEngine {
     __syncwarp();
   }
 
-  __device__ __forceinline__ void flush(float* buf, float2* ml, int, int lane) const {
+  __device__ __forceinline__ void flush(float* buf, int, int lane) const {
 #pragma unroll
     for (int i = 0; i < kRows / 2; ++i) {
       float sum = l[i];
 #pragma unroll
       for (int x = 2; x < 32; x <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      if (lane < 2) ml[2 * i + lane] = make_float2(lane ? m[2 * i + 1] : m[2 * i], sum);
+      if (lane < 2) row_stats(buf, 2 * i + lane) = make_float2(lane ? m[2 * i + 1] : m[2 * i], sum);
     }
 #pragma unroll
     for (int r = 0; r < kRows; ++r) *reinterpret_cast<float4*>(buf + r * kPadRow + 4 * lane) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
@@ -533,19 +547,18 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
   constexpr int kThreads = E::kWarps * 32, kBufRow = 8 * kPadRow;
   unsigned char* const stages = smem;                                               // [kWarps][kStages][kStageBytes]
   float* const buf = reinterpret_cast<float*>(smem + E::kWarps * E::kStages * E::kStageBytes);   // [kWarps][8][kPadRow]
-  float2* const ml = reinterpret_cast<float2*>(buf + E::kWarps * kBufRow);          // [kWarps][8]
-  unsigned char* const extra = reinterpret_cast<unsigned char*>(ml + E::kWarps * 8);
-  __shared__ int64_t before[kMaxBatch + 1];                              // tiles of the sequences before
+  unsigned char* const extra = reinterpret_cast<unsigned char*>(buf + E::kWarps * kBufRow);
+  __shared__ Plan plan;
   __shared__ int last_here;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_trigger();
 
-  if (warp == 0) count_tiles<E>(a, before, lane);
+  if (warp == 0) make_plan<E>(a, plan, lane);
   __syncthreads();
   Run run;
   Part c;
-  if (!take_run<E>(a, before, run, c)) return;
+  if (!take_run<E>(a, plan, run, c)) return;
 
   // Copies run kStages - 1 tiles ahead of the products, into the next units where these end.
   Part p = c;
@@ -555,32 +568,36 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
   auto bytes = [](int64_t channels) { return kShift < 0 ? channels >> 1 : channels << (kShift < 0 ? 0 : kShift); };
   const int64_t page_bytes = bytes(a.pg.page_stride);
   const uint32_t in_page = (1u << a.pg.page_shift) - 1u;
-  int left = 0, base_p = 0, page[E::kSub] = {};
+  // Pages are looked up by the lanes, lane l that of piece l % kSub of tile l / kSub ahead, 32 / kSub tiles at a time and these again as long
+  // before their use.
+  constexpr int kWindow = 32 / E::kSub, kShort = 4;
+  int left = 0, base_p = 0, seen = 0, pages = 0, pages_next = 0;
   int64_t head_bytes = 0;
   const int32_t* table = nullptr;
   uint32_t bad = 0;                                                       // pieces of stages whose page does not exist
   bool more = true;
-  auto look_up = [&] {                                                    // (a tile before its use)
-#pragma unroll
-    for (int b = 0; b < E::kSub; ++b)
-      if (base_p + 16 * b < p.u.limit) page[b] = __ldg(table + ((base_p + 16 * b) >> a.pg.page_shift));
+  auto look_up = [&](int base) {
+    const int row = base + (lane / E::kSub) * E::kTile + (lane % E::kSub) * 16;
+    return row >= 0 && row < p.u.limit ? __ldg(table + (row >> a.pg.page_shift)) : 0;
   };
   auto enter = [&] {
     left = (int)(p.end - p.begin);
     base_p = (int)(p.begin - p.unit_begin) * E::kTile + warp * (16 * E::kSub);
     head_bytes = bytes(p.u.h * a.pg.head_stride);
     table = a.pg.table + (int64_t)p.u.b * a.pg.table_stride;
-    look_up();
+    seen = 0;
+    pages = look_up(base_p);
+    if (left > kWindow) pages_next = look_up(base_p + kWindow * E::kTile);
   };
   auto produce = [&](int slot) {
     if (more) {
       bad &= ~(((1u << E::kSub) - 1u) << (slot * E::kSub));
 #pragma unroll
       for (int b = 0; b < E::kSub; ++b) {
-        const int row = base_p + 16 * b;
+        const int row = base_p + 16 * b, page = __shfl_sync(0xffffffffu, pages, seen * E::kSub + b);
         if (row < p.u.limit) {
-          if ((unsigned)page[b] < (unsigned)a.pg.n_pages) {
-            E::issue(a, ln, mine + slot * E::kStageBytes + b * E::kSubBytes, page[b] * page_bytes + head_bytes + (int64_t)(row & in_page) * ln.rows, lane);
+          if ((unsigned)page < (unsigned)a.pg.n_pages) {
+            E::issue(a, ln, mine + slot * E::kStageBytes + b * E::kSubBytes, page * page_bytes + head_bytes + (int64_t)(row & in_page) * ln.rows, lane);
           } else {
             bad |= 1u << (slot * E::kSub + b);
             if (lane == 0) atomicOr(a.status, kStatusBadPage);
@@ -589,10 +606,12 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
       }
       base_p += E::kTile;
       if (--left == 0) {
-        more = next<E>(a, p, before, run.end);
+        more = next<E>(a, plan, run, p);
         if (more) enter();
-      } else {
-        look_up();
+      } else if (++seen == kWindow) {
+        seen = 0;
+        pages = pages_next;
+        if (left > kWindow) pages_next = look_up(base_p + kWindow * E::kTile);
       }
     }
     ptx::cp_async_commit();
@@ -602,7 +621,7 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
 
   E e;
   int slot = 0, ahead = E::kStages - 1;
-  for (bool on = true; on; on = next<E>(a, c, before, run.end)) {
+  for (bool on = true; on; on = next<E>(a, plan, run, c)) {
     e.begin(a, c.u, extra, warp, lane);
     int base = (int)(c.begin - c.unit_begin) * E::kTile + warp * (16 * E::kSub);
 #pragma unroll 1
@@ -611,11 +630,9 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
       ptx::cp_async_wait<E::kStages - 1>();
       __syncwarp();
       const uint32_t stage = mine + slot * E::kStageBytes, gone = (bad >> (slot * E::kSub)) & ((1u << E::kSub) - 1u);
-      if (base + 16 * E::kSub <= c.u.full && gone == 0u) {
-        e.template step<true>(a, c.u, stage, base, extra, warp, lane);
-      } else if (base < c.u.limit) {
-        e.template step<false>(a, c.u, stage, base, extra, warp, lane, gone);
-      }
+      // (a short part keeps to the code that its last tile needs anyway: it would wait for the other's to be fetched)
+      if (c.end - c.begin > kShort && base + 16 * E::kSub <= c.u.full && gone == 0u) e.template step<true>(a, c.u, stage, base, 0u, extra, warp, lane);
+      else if (base < c.u.limit) e.template step<false>(a, c.u, stage, base, gone, extra, warp, lane);
       __syncwarp();
       ahead = slot;
       slot = slot + 1 == E::kStages ? 0 : slot + 1;
@@ -624,18 +641,19 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
     const Share<E> share(a, run, c);
     for (int nt = 0; nt < E::kNT; ++nt) {
       __syncthreads();
-      e.flush(buf + warp * kBufRow, ml + warp * 8, nt, lane);
+      e.flush(buf + warp * kBufRow, nt, lane);
       __syncthreads();
       for (int r = warp; r < 8; r += E::kWarps) {
         float top = kLowest, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < E::kWarps; ++w) top = fmaxf(top, ml[w * 8 + r].x);
+        for (int w = 0; w < E::kWarps; ++w) top = fmaxf(top, row_stats(buf + w * kBufRow, r).x);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < E::kWarps; ++w) {
-          const float f = ex2(ml[w * 8 + r].x - top);
+          const float2 stat = row_stats(buf + w * kBufRow, r);
+          const float f = ex2(stat.x - top);
           const float4 x = *reinterpret_cast<const float4*>(buf + w * kBufRow + r * kPadRow + 4 * lane);
-          sum = fmaf(f, ml[w * 8 + r].y, sum);
+          sum = fmaf(f, stat.y, sum);
           acc = make_float4(fmaf(f, x.x, acc.x), fmaf(f, x.y, acc.y), fmaf(f, x.z, acc.z), fmaf(f, x.w, acc.w));
         }
         if (share.alone) {
@@ -664,7 +682,7 @@ paged_attend_kernel(const __grid_constant__ Attend a) {
 
 template <class E>
 cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
-  constexpr int smem = E::kWarps * (E::kStages * E::kStageBytes + 8 * kPadRow * 4 + 64) + E::kExtra;
+  constexpr int smem = E::kWarps * (E::kStages * E::kStageBytes + 8 * kPadRow * 4) + E::kExtra;
   cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(paged_attend_kernel<E>, dim3((unsigned)most_ctas<E>(a, n_sm)), dim3(E::kWarps * 32), smem, s, 1, a);

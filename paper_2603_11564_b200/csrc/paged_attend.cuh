@@ -50,6 +50,17 @@ struct Unit {
   int full;                // end of the rows that all of them see
 };
 
+// What a CTA works out at its start, in shared memory: the tiles before each sequence, and the lengths.
+struct Plan {
+  int64_t before[kMaxBatch + 1];
+  int32_t held[kMaxBatch];
+};
+
+// 64-bit division takes ten times as long as 32-bit, which nearly always does.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 // Tiles of a sequence's units, and their number.
 template <class E>
 __device__ __forceinline__ int tiles_of(const Attend& a, int b, int held, int* units) {
@@ -66,20 +77,28 @@ struct Part {
   Unit u;
 };
 
+// A CTA's run.  Runs are equal, cut in proportion (units of one length that divide the CTAs evenly are not cut across), and of kMinRun tiles at
+// least: below that, a CTA more costs more (its part is written, and read by another) than it saves.
+struct Run {
+  int64_t begin, end, total, ctas;
+  __device__ __forceinline__ int64_t start(int64_t cta) const { return quotient(total * cta, ctas); }
+  __device__ __forceinline__ int64_t cta_of(int64_t tile) const { return quotient((tile + 1) * ctas - 1, total); }
+};
+
 template <class E>
-__device__ __forceinline__ void place(const Attend& a, Part& p, int b, int unit, int64_t unit_begin, int64_t begin, int64_t run_end) {
-  const int n = a.n[b], held = a.pg.len[b];
+__device__ __forceinline__ void place(const Attend& a, const Plan& plan, const Run& run, Part& p, int b, int unit, int64_t unit_begin) {
+  const int n = a.n[b], held = plan.held[b];
   int units;
   p.tiles = tiles_of<E>(a, b, held, &units);
   p.unit = unit;
   p.unit_begin = unit_begin;
-  p.begin = begin;
-  p.end = min(run_end, unit_begin + p.tiles);
+  p.begin = max(run.begin, unit_begin);
+  p.end = min(run.end, unit_begin + p.tiles);
   Unit& u = p.u;
   u.b = b;
   u.rows = n * a.group;
-  const int row_tiles = units / a.n_kv_heads;
-  u.h = unit / row_tiles;
+  const int row_tiles = (u.rows + E::kRows - 1) / E::kRows;
+  u.h = row_tiles == 1 ? unit : unit / row_tiles;
   u.row0 = (unit - u.h * row_tiles) * E::kRows;
   u.held = held;
   const int64_t room = (int64_t)a.pg.table_stride << a.pg.page_shift;
@@ -87,20 +106,19 @@ __device__ __forceinline__ void place(const Attend& a, Part& p, int b, int unit,
   u.limit = held < 0 ? 0 : (int)min((int64_t)held + last + 1, room);
   u.full = held < 0 ? 0 : (int)min((int64_t)held + first + 1, room);
 }
-// The part of the run behind p, if there is one.
+// The part of the run before p, if there is one.  A run is walked from its last part to its first: the last is the beginning of a unit whose other
+// CTAs take as long as this one, so a CTA that did it at the end, behind a join of the unit before, would keep that unit waiting.
 template <class E>
-__device__ __forceinline__ bool next(const Attend& a, Part& p, const int64_t* before, int64_t run_end) {
-  if (p.end >= run_end) {
-    p.begin = p.end;
-    return false;
+__device__ __forceinline__ bool next(const Attend& a, const Plan& plan, const Run& run, Part& p) {
+  if (p.unit_begin <= run.begin) return false;
+  int b = p.u.b, unit = p.unit - 1;
+  if (unit < 0) {
+    do --b; while (plan.before[b] >= p.unit_begin);
+    tiles_of<E>(a, b, plan.held[b], &unit);
+    --unit;
   }
-  const int64_t at = p.end;                          // (the part ended with its unit)
-  int b = p.u.b, unit = p.unit + 1;
-  if (at >= before[b + 1]) {
-    unit = 0;
-    do ++b; while (before[b + 1] <= at);
-  }
-  place<E>(a, p, b, unit, at, at, run_end);
+  int units;
+  place<E>(a, plan, run, p, b, unit, p.unit_begin - tiles_of<E>(a, b, plan.held[b], &units));
   return true;
 }
 // Rows that query row r of the unit sees.
@@ -132,33 +150,38 @@ __device__ __forceinline__ void write_row(const Attend& a, const Unit& u, int r,
 }
 
 // Row r of a unit from the partial results of n CTAs, in their order: the first one's at `first`, the x-th one's at others + 2 x slots.  What a
-// warp waits for is latency, so its loads are in flight together: all maxima and sums, and kBatch outputs at a time.
+// warp waits for is latency, so its loads are in flight together: maxima and sums, and kBatch outputs at a time.
 template <class E>
 __device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r, const float* first, const float* others, int n, int lane) {
-  constexpr int kBatch = 16;
+  constexpr int kBatch = E::kMergeBatch;
   auto from = [&](int x) { return x == 0 ? first : others + 2 * (int64_t)x * kSlotFloats<E>; };
   auto stats = [&](int x) {
     return x < n ? __ldcg(reinterpret_cast<const float2*>(from(x) + E::kSlotRows * kHeadDim) + r) : make_float2(kLowest, 0.f);
   };
-  const float2 st0 = stats(lane), st1 = stats(32 + lane);
-  float top = fmaxf(st0.x, st1.x), sum = 0.f;
+  float4 v[kBatch];
+  auto load = [&](int x0) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+      if (x0 + i < n) v[i] = __ldcg(reinterpret_cast<const float4*>(from(x0 + i) + r * kHeadDim) + lane);
+  };
+  float2 st = stats(lane);
+  float top = fmaxf(st.x, stats(32 + lane).x), sum = 0.f;
+  load(0);
   for (int x = 64 + lane; x < n; x += 32) top = fmaxf(top, stats(x).x);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
   for (int x0 = 0; x0 < n; x0 += 32) {
-    const float2 st = x0 == 0 ? st0 : x0 == 32 ? st1 : stats(x0 + lane);
+    if (x0 > 0) st = stats(x0 + lane);
     const float weight = x0 + lane < n ? ex2(st.x - top) : 0.f;
     sum = fmaf(weight, st.y, sum);
 #pragma unroll 1
     for (int h = 0; h < min(32, n - x0); h += kBatch) {
-      float4 v[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(from(min(x0 + h + i, n - 1)) + r * kHeadDim) + lane);
+      if (x0 + h > 0) load(x0 + h);
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const float f = __shfl_sync(0xffffffffu, weight, (h + i) & 31);
+        const float f = __shfl_sync(0xffffffffu, weight, h + i);
         if (x0 + h + i < n) acc = make_float4(fmaf(f, v[i].x, acc.x), fmaf(f, v[i].y, acc.y), fmaf(f, v[i].z, acc.z), fmaf(f, v[i].w, acc.w));
       }
     }
@@ -169,50 +192,49 @@ __device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r,
 }
 
 
-// Tiles before each sequence, by one warp.
+// The plan, by one warp.
 template <class E>
-__device__ __forceinline__ void count_tiles(const Attend& a, int64_t* before, int lane) {
+__device__ __forceinline__ void make_plan(const Attend& a, Plan& plan, int lane) {
   int64_t run = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     int units = 0, tiles = 0;
     const int b = b0 + lane;
     if (b < a.batch) {
       const int held = a.pg.len[b];
+      plan.held[b] = held;
       tiles = tiles_of<E>(a, b, held, &units);
       if (blockIdx.x == 0 && tiles > 0 && (int64_t)held + a.n[b] > (int64_t)a.pg.table_stride << a.pg.page_shift) atomicOr(a.status, kStatusBadPage);
     }
     int64_t x = (int64_t)tiles * units;
+    if (a.batch > 1) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
-      if (lane >= d) x += y;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
     }
-    if (b < a.batch) before[b + 1] = run + x;
+    if (b < a.batch) plan.before[b + 1] = run + x;
     run += __shfl_sync(0xffffffffu, x, 31);
   }
-  if (lane == 0) before[0] = 0;
+  if (lane == 0) plan.before[0] = 0;
 }
 
-// A CTA's run, and its first part.  Runs are equal, and of kMinRun tiles at least: below that, a CTA more costs more (its part is written,
-// and read by another) than it saves.
-struct Run {
-  int64_t total, ctas, begin, end;
-};
+// The CTA's run, and the last part of it.
 template <class E>
-__device__ __forceinline__ bool take_run(const Attend& a, const int64_t* before, Run& run, Part& c) {
-  run.total = before[a.batch];
+__device__ __forceinline__ bool take_run(const Attend& a, const Plan& plan, Run& run, Part& c) {
+  run.total = plan.before[a.batch];
   run.ctas = max((int64_t)1, min((int64_t)gridDim.x, run.total / E::kMinRun));
   if (blockIdx.x >= run.ctas) return false;
-  run.begin = run.total * blockIdx.x / run.ctas;
-  run.end = run.total * (blockIdx.x + 1) / run.ctas;
+  run.begin = run.start(blockIdx.x);
+  run.end = run.start(blockIdx.x + 1);
   int lo = 0, hi = a.batch - 1, units;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (before[mid] <= run.begin) lo = mid; else hi = mid - 1;
+    if (plan.before[mid] < run.end) lo = mid; else hi = mid - 1;
   }
-  const int tiles = tiles_of<E>(a, lo, a.pg.len[lo], &units);
-  const int unit = (int)((run.begin - before[lo]) / tiles);
-  place<E>(a, c, lo, unit, before[lo] + (int64_t)unit * tiles, run.begin, run.end);
+  const int tiles = tiles_of<E>(a, lo, plan.held[lo], &units);
+  const int unit = (int)quotient(run.end - 1 - plan.before[lo], tiles);
+  place<E>(a, plan, run, c, lo, unit, plan.before[lo] + (int64_t)unit * tiles);
   return true;
 }
 // Whether the run covers a part's whole unit; else the CTAs that share it, and this one's slot.
@@ -225,11 +247,15 @@ struct Share {
   __device__ __forceinline__ Share(const Attend& a, const Run& run, const Part& c) {
     const int64_t unit_end = c.unit_begin + c.tiles;
     alone = c.unit_begin >= run.begin && unit_end <= run.end;
-    c0 = ((c.unit_begin + 1) * run.ctas - 1) / run.total;
-    n = (int)((unit_end * run.ctas - 1) / run.total - c0) + 1;
+    c0 = blockIdx.x;
+    n = 1;
+    mine = first = others = nullptr;
+    if (alone) return;
+    c0 = run.cta_of(c.unit_begin);
+    n = (int)(run.cta_of(unit_end - 1) - c0) + 1;
     mine = a.part + (2 * (int64_t)blockIdx.x + (c.unit_begin > run.begin ? 1 : 0)) * kSlotFloats<E>;
     others = a.part + 2 * c0 * kSlotFloats<E>;
-    first = others + (c.unit_begin > run.total * c0 / run.ctas ? kSlotFloats<E> : 0);     // (behind another one of that CTA's own)
+    first = others + (c.unit_begin > run.start(c0) ? kSlotFloats<E> : 0);                 // (behind another one of that CTA's own)
   }
 };
 // No more CTAs than there can be tiles.

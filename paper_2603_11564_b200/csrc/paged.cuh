@@ -84,9 +84,17 @@ __device__ __forceinline__ uint32_t scale_bits(float s, float* value) {
   *value = tiny ? low - 24576.f : __uint_as_float(u << 20);
   return tiny ? __float_as_uint(low) & 15u : u - (120u << 3);
 }
-// The nearest e2m1 to y in 0 .. 6, ties to even: a sum whose last bit is the step of y's range leaves the code in its last three.
-__device__ __forceinline__ uint32_t code_bits(float y) {
-  return __float_as_uint(y + (y < 2.f ? 6291456.f : y < 4.f ? 12582914.f : 25165832.f)) & 7u;
+// The nearest e2m1 to each of eight values, ties to even, the largest beyond it: channel i in bits 4 i .. 4 i + 3.
+__device__ __forceinline__ uint32_t codes_of(const float2 (&y)[4]) {
+  uint32_t w;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+      : "=r"(w) : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
+  return w;
 }
 
 }  // namespace dapq

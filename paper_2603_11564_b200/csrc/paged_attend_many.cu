@@ -26,13 +26,14 @@ struct Smem {
   static constexpr int q = 0, k = 2 * kTileBytes, v = k + kRing * kTileBytes, bars = v + kRing * kTileBytes;
   // barriers
   static constexpr int k_full = 0, k_empty = 2, v_full = 4, v_empty = 6, q_full = 8, s_full = 10, p_half = 12, p_full = 14, pv_done = 16, drain = 18, n_bars = 20;   // (one unused: the plan lies on 16 bytes)
-  static constexpr int plan = bars + 8 * n_bars, tmem_ptr = plan + (int)sizeof(Plan), abort_flag = tmem_ptr + 4, last_here = abort_flag + 4,
+  static constexpr int plan = bars + 8 * n_bars, run = plan + (int)sizeof(Plan), parts = run + (int)sizeof(Run), tmem_ptr = parts + (kThreads / 32) * (int)sizeof(Part), abort_flag = tmem_ptr + 4, last_here = abort_flag + 4,
                        total = last_here + 4;
 };
 static_assert(Smem::total <= 232448, "exceeds the shared memory a CTA can opt in to");
 
 struct Many {                                         // geometry, for the shared scheduling
   static constexpr int kRows = 256, kSlotRows = 256, kTile = 128, kCtas = 1, kMinRun = 4;
+  static constexpr bool kFromEnd = false;
   using T = __nv_bfloat16;
   __device__ __forceinline__ static int channel(int p) { return p; }
 };
@@ -76,6 +77,15 @@ __device__ __forceinline__ uint32_t pack(bool f16, float x, float y) {
   }
   const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A warp's next part.  Its parts and the CTA's run lie in shared memory: in registers they left too few for the softmax.
+__device__ __forceinline__ bool next_part(const Attend& a, const Plan& plan, const Run& run, Part& c, int lane) {
+  __syncwarp();
+  int on = 0;
+  if (lane == 0) on = next<Many>(a, plan, run, c);
+  __syncwarp();
+  return __shfl_sync(0xffffffffu, on, 0) != 0;
 }
 
 struct Wait {
@@ -127,10 +137,10 @@ __device__ __forceinline__ void store_codes(uint32_t tile, int r, const Codes& c
 
 // Keys go one tile ahead of the values: tile t's second product and tile t + 1's first follow one another.
 template <bool kFp4>
-__device__ __forceinline__ void produce(const Attend& a, Part c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase) {
+__device__ __forceinline__ void produce(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase) {
   const int tid = threadIdx.x - 256, lane = tid & 31, warp = tid >> 5;
   int done = 0;                                                           // tiles so far
-  for (bool on = true; on; on = next<Many>(a, plan, run, c)) {
+  for (bool on = true; on; on = next_part(a, plan, run, c, lane)) {
     const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile;
     auto offset = [&](int pages, int base, int r) {                       // channel offset of row r of a tile, negative: reads as zero
       const int pg = __shfl_sync(0xffffffffu, pages, r >> 4);
@@ -219,8 +229,9 @@ __device__ __forceinline__ bool elect_one() {
 // A whole warp walks the tiles, one of its lanes issues: what the instructions take is then uniform, and stays in uniform registers.  (With the
 // walk in one lane's branch every operand was moved there for every MMA, and issuing, not the products, set the pace: 120 cycles each.)
 template <bool kFp4>
-__device__ __forceinline__ void issue(const Attend& a, Part c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase, uint32_t tmem) {
+__device__ __forceinline__ void issue(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase, uint32_t tmem) {
   constexpr uint32_t idesc_s = kFp4 ? umma_idesc_f16(128, 128) : umma_idesc(128, 128), idesc_o = idesc_s | (1u << 16);   // (V: MN-major)
+  const int lane = threadIdx.x & 31;
   uint32_t done = 0, parts = 0, parts_b = 0, done_b = 0;
   bool ok = true;
   auto commit = [&](int i) {
@@ -246,7 +257,7 @@ __device__ __forceinline__ void issue(const Attend& a, Part c, const Plan& plan,
     }
     __syncwarp();
   };
-  for (bool on = true; on && ok; on = next<Many>(a, plan, run, c)) {
+  for (bool on = true; on && ok; on = next_part(a, plan, run, c, lane)) {
     const int n = __shfl_sync(0xffffffffu, (int)(c.end - c.begin), 0);
     const bool two = __shfl_sync(0xffffffffu, c.u.rows - c.u.row0, 0) > 128;
     ok = wait.warp(Smem::q_full, parts & 1) && (!two || wait.warp(Smem::q_full + 1, parts_b & 1)) && wait.warp(Smem::k_full + (done & 1), (done >> 1) & 1);
@@ -335,7 +346,7 @@ __device__ __forceinline__ void merge_rows(const Attend& a, const Unit& u, const
   }
 }
 template <bool kFp4, bool kCap>
-__device__ __forceinline__ void softmax(const Attend& a, Part c, const Plan& plan, const Run& run, const Wait& wait, uint8_t* smem, uint32_t sbase,
+__device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint8_t* smem, uint32_t sbase,
                                         uint32_t tmem) {
   using E = ManyOf<kFp4>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = warp >> 2, r = threadIdx.x & 127;
@@ -344,7 +355,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part c, const Plan& pla
   int done = 0;                                                           // tiles of this half so far
   bool ok = true;
   // (an aborting warp still walks every part: the others wait for it at the barriers, and the arrival counters have to come back to 0)
-  for (bool on = true; on; on = next<Many>(a, plan, run, c)) {
+  for (bool on = true; on; on = next_part(a, plan, run, c, lane)) {
     const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile, row = c.u.row0 + x * 128 + r;
     const bool mine = x == 0 || c.u.rows - c.u.row0 > 128;                // (tile B of a unit of 128 rows or fewer has none)
     float m = kLowest, l = 0.f;
@@ -538,9 +549,16 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + Smem::tmem_ptr);
-  Run run;
-  Part c;
-  if (take_run<Many>(a, plan, run, c)) {
+  Run& run = *reinterpret_cast<Run*>(smem + Smem::run);
+  Part& c = reinterpret_cast<Part*>(smem + Smem::parts)[warp];
+  int mine = 0;
+  if (lane == 0) {
+    Run r;
+    mine = take_run<Many>(a, plan, r, c);
+    if (warp == 0) run = r;
+  }
+  __syncthreads();
+  if (__shfl_sync(0xffffffffu, mine, 0)) {
     // registers: 256 x 184 + 128 x 88 + 128 x 56, the 65536 that the block was launched with
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");

@@ -11,7 +11,7 @@ constexpr int kStoreThreads = 256, kHalf = kHeadDim / 2;
 // A thread holds kPer consecutive channels of either half of a row, 64 / kPer threads a row: 4 where rows are copied (16-byte pieces
 // of fp32, the most threads), 16 where they become 4 bits, so that a thread has two whole groups.
 template <bool kFp4> constexpr int kPerOf = kFp4 ? 16 : 4;
-template <int kPer> struct Row { float lo[kPer], hi[kPer]; };
+template <int kPer> struct Row { float2 lo[kPer / 2], hi[kPer / 2]; };           // channel pairs, for the packed fp32 instructions
 template <typename T, int kPer> struct Raw { uint4 w[kPer * sizeof(T) / 8]; };      // (both halves)
 
 template <typename T, int kPer>
@@ -34,45 +34,62 @@ template <typename T, int kPer>
 __device__ __forceinline__ Row<kPer> widen_row(const Raw<T, kPer>& r) {
   Row<kPer> x;
   const uint32_t* w = reinterpret_cast<const uint32_t*>(r.w);
-  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      x.lo[i] = __uint_as_float(w[i]);
-      x.hi[i] = __uint_as_float(w[kPer + i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kPer / 2; ++i) {
-      x.lo[2 * i] = __uint_as_float(w[i] << 16);
-      x.lo[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      x.hi[2 * i] = __uint_as_float(w[kPer / 2 + i] << 16);
-      x.hi[2 * i + 1] = __uint_as_float(w[kPer / 2 + i] & 0xffff0000u);
+  for (int i = 0; i < kPer / 2; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      x.lo[i] = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+      x.hi[i] = make_float2(__uint_as_float(w[kPer + 2 * i]), __uint_as_float(w[kPer + 2 * i + 1]));
+    } else {
+      x.lo[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+      x.hi[i] = make_float2(__uint_as_float(w[kPer / 2 + i] << 16), __uint_as_float(w[kPer / 2 + i] & 0xffff0000u));
     }
   }
   return x;
 }
-__device__ __forceinline__ void store4(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* x) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+__device__ __forceinline__ void store4(float* p, float2 a, float2 b) { *reinterpret_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float2 x, float2 y) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(y.x, y.y);
   *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+// The larger of a, |b| and |c|; NaN if one is.
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
 }
 
 // A group of 16 channels in 4 bits.  Every rounding is that of the formula: the quotients x / (scale kappa) are correctly rounded
 // (reciprocal, product and one correction by the exact remainder, after Markstein 1990), so ties go where they would in exact
-// arithmetic whenever scale kappa is exact.  Magnitudes are clamped to the largest code's first, which keeps the remainder finite.
-__device__ __forceinline__ void store_group(char* codes, unsigned char* scale, float kappa, const float* x) {
-  uint32_t top = 0;
+// arithmetic whenever scale kappa is exact.
+__device__ __forceinline__ void store_group(char* codes, unsigned char* scale, float kappa, const float2* in) {
+  float2 x[8];
+  float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);     // (NaN above infinity above all numbers)
-  const bool fine = top < 0x7f800000u;
+  for (int i = 0; i < 8; ++i) {
+    x[i] = in[i];
+    top = largest(top, x[i].x, x[i].y);
+  }
+  const bool fine = top < __uint_as_float(0x7f800000u);
+  const float ratio = __fdiv_rn(fine ? top : 0.f, __fmul_rn(6.f, kappa));
   float s;
-  const uint32_t bits = scale_bits(fminf(__fdiv_rn(__uint_as_float(fine ? top : 0u), __fmul_rn(6.f, kappa)), 448.f), &s);
-  const float step = __fmul_rn(s, kappa), most = 6.f * step, r = step > 0.f ? __frcp_rn(step) : 0.f;   // (all codes 0 without a scale)
-  uint32_t w[2] = {0u, 0u};
+  const uint32_t bits = scale_bits(fminf(ratio, 448.f), &s);
+  const float step = __fmul_rn(s, kappa), r = step > 0.f ? __frcp_rn(step) : 0.f;       // (all codes 0 without a scale)
+  if (!(ratio <= 448.f)) {                                                // (magnitudes where the largest code holds: their quotients stay finite)
+    const float most = 6.f * step;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float v = fminf(fabsf(x[i]), most), q = __fmul_rn(v, r), y = __fmaf_rn(__fmaf_rn(-q, step, v), r, q);
-    w[i / 8] |= (code_bits(y) | ((__float_as_uint(x[i]) >> 28) & 8u)) << (4 * (i & 7));
+    for (int i = 0; i < 8; ++i) x[i] = make_float2(fminf(fmaxf(x[i].x, -most), most), fminf(fmaxf(x[i].y, -most), most));
+  }
+  const float2 rr = make_float2(r, r), minus = make_float2(-step, -step);
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float2 y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = x[4 * h + i], q = __fmul2_rn(v, rr);
+      y[i] = __ffma2_rn(__ffma2_rn(q, minus, v), rr, q);
+    }
+    w[h] = codes_of(y);
   }
   *reinterpret_cast<uint2*>(codes) = fine ? make_uint2(w[0], w[1]) : make_uint2(0u, 0u);
   *scale = fine ? (unsigned char)bits : (unsigned char)0x7f;
@@ -85,34 +102,34 @@ __device__ __forceinline__ void store_row(char* base, unsigned char* scales, flo
     store_group(base + off / 2 + 8 * lane, scales + off / 16 + lane, kappa, x.lo);
     store_group(base + off / 2 + 32 + 8 * lane, scales + off / 16 + 4 + lane, kappa, x.hi);
   } else {
-    store4(reinterpret_cast<T*>(base) + off + 4 * lane, x.lo);
-    store4(reinterpret_cast<T*>(base) + off + kHalf + 4 * lane, x.hi);
+    store4(reinterpret_cast<T*>(base) + off + 4 * lane, x.lo[0], x.lo[1]);
+    store4(reinterpret_cast<T*>(base) + off + kHalf + 4 * lane, x.hi[0], x.hi[1]);
   }
 }
 
-// The rotation in fp32, every product and sum rounded by itself: what a user's own elementwise rotation gives, bit for bit.
-__device__ __forceinline__ float turn_lo(float lo, float hi, float2 cs) { return __fsub_rn(__fmul_rn(lo, cs.x), __fmul_rn(hi, cs.y)); }
-__device__ __forceinline__ float turn_hi(float lo, float hi, float2 cs) { return __fadd_rn(__fmul_rn(hi, cs.x), __fmul_rn(lo, cs.y)); }
+// The rotation in fp32, every product and sum rounded by itself: what a user's own elementwise rotation gives, bit for bit.  cos, sin: of the
+// row's token, [d / 2].
+struct Angles { float cs[kHalf], sn[kHalf]; };
 template <int kPer>
-__device__ __forceinline__ void rotate(Row<kPer>& x, const float2* cs, int lane, int interleaved) {
+__device__ __forceinline__ void rotate(Row<kPer>& x, const Angles& an, int lane, int interleaved) {
   if (interleaved) {
-    float* half[2] = {x.lo, x.hi};
+    float2* half[2] = {x.lo, x.hi};
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int p = 0; p < kPer / 2; ++p) {
-        const float2 a = cs[kHalf / 2 * h + kPer / 2 * lane + p];
-        const float lo = half[h][2 * p], hi = half[h][2 * p + 1];
-        half[h][2 * p] = turn_lo(lo, hi, a);
-        half[h][2 * p + 1] = turn_hi(lo, hi, a);
+        const int at = kHalf / 2 * h + kPer / 2 * lane + p;
+        const float c = an.cs[at], s = an.sn[at];
+        const float2 a = __fmul2_rn(half[h][p], make_float2(c, c)), b = __fmul2_rn(half[h][p], make_float2(s, s));
+        half[h][p] = __fadd2_rn(a, make_float2(-b.y, b.x));
       }
   } else {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const float2 a = cs[kPer * lane + i];
-      const float lo = x.lo[i], hi = x.hi[i];
-      x.lo[i] = turn_lo(lo, hi, a);
-      x.hi[i] = turn_hi(lo, hi, a);
+    for (int i = 0; i < kPer / 2; ++i) {
+      const float2 c = *reinterpret_cast<const float2*>(an.cs + kPer * lane + 2 * i), s = *reinterpret_cast<const float2*>(an.sn + kPer * lane + 2 * i);
+      const float2 lo = x.lo[i], hi = x.hi[i];
+      x.lo[i] = __ffma2_rn(__fmul2_rn(hi, s), make_float2(-1.f, -1.f), __fmul2_rn(lo, c));     // (a difference: the product by -1 is exact)
+      x.hi[i] = __fadd2_rn(__fmul2_rn(hi, c), __fmul2_rn(lo, s));
     }
   }
 }
@@ -123,7 +140,7 @@ template <typename T, bool kFp4, int kTok>
 __global__ void __launch_bounds__(kStoreThreads)
 paged_append_kernel(const __grid_constant__ PagedDev pg, const __grid_constant__ NewRows t, const __grid_constant__ NewTokensDev nt,
                     const double* __restrict__ inv_freq, int n_kv_heads, int n_q_heads, int interleaved, int* __restrict__ status) {
-  __shared__ float2 angle[kTok][kHalf];
+  __shared__ __align__(16) Angles angle[kTok];
   __shared__ int seq[kTok];
   __shared__ int64_t place[kTok];
   const int tok0 = blockIdx.x * kTok, n = min(kTok, t.cu[t.batch] - tok0);
@@ -143,7 +160,8 @@ paged_append_kernel(const __grid_constant__ PagedDev pg, const __grid_constant__
     for (int a = threadIdx.x; a < n * kHalf; a += kStoreThreads) {
       double sn, cs;
       sincos((double)nt.positions[tok0 + a / kHalf] * inv_freq[a % kHalf], &sn, &cs);
-      angle[a / kHalf][a % kHalf] = make_float2((float)cs, (float)sn);
+      angle[a / kHalf].cs[a % kHalf] = (float)cs;
+      angle[a / kHalf].sn[a % kHalf] = (float)sn;
     }
   __syncthreads();
   {
@@ -294,8 +312,8 @@ paged_read_kernel(const __grid_constant__ PagedDev pg, const __grid_constant__ R
           for (int w = 0; w < 4; ++w) z[w] = __floats2bfloat162_rn(y[2 * w], y[2 * w + 1]);
           *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(z);
         } else {
-          store4(out, y);
-          store4(out + 4, y + 4);
+          store4(out, make_float2(y[0], y[1]), make_float2(y[2], y[3]));
+          store4(out + 4, make_float2(y[4], y[5]), make_float2(y[6], y[7]));
         }
       } else {
 #pragma unroll

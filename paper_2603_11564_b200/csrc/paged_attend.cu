@@ -79,7 +79,7 @@ template <bool kFp4, int kTiles>
 struct TensorEngine {
   static constexpr int kNT = kTiles;
   static constexpr int kWarps = 8, kSub = kFp4 && kNT == 1 ? 2 : 1, kTile = kWarps * kSub * 16, kRows = 8 * kNT, kSlotRows = 16, kMergeBatch = 16, kCtas = 1, kStages = kFp4 ? 4 : 3;
-  static constexpr bool kFromEnd = true;
+  static constexpr bool kFromEnd = true, kEven = true;
   static constexpr int kMinRun = 4, kByteShift = kFp4 ? -1 : 1, kSubBytes = kFp4 ? 16 * 144 : 16 * 512, kStageBytes = kSub * kSubBytes;
   static constexpr int kExtra = 0;
   static constexpr float kLift = kFp4 ? 11.f : 0.f;
@@ -376,7 +376,7 @@ template <bool kFp4>
 struct FloatEngine {
   static constexpr int kWarps = 4, kSub = 1, kTile = kWarps * 16, kRows = 8, kSlotRows = 16, kMergeBatch = 16, kCtas = kFp4 ? 2 : 1, kStages = kFp4 ? 4 : 3, kMinRun = 1, kByteShift = kFp4 ? -1 : 2;
   static constexpr int kSubBytes = kFp4 ? 16 * 144 : 16 * 1024, kStageBytes = kSubBytes;
-  static constexpr bool kFromEnd = true;
+  static constexpr bool kFromEnd = true, kEven = false;
   static constexpr int kQBytes = kRows * kHeadDim * 4, kPBytes = 16 * kRows * 4;
   static constexpr int kExtra = kQBytes + kWarps * kPBytes;
   static constexpr float kLift = 0.f;

@@ -54,6 +54,7 @@ struct Unit {
 struct Plan {
   int64_t before[kMaxBatch + 1];
   int32_t held[kMaxBatch];
+  int64_t units;
 };
 
 // 64-bit division takes ten times as long as 32-bit, which nearly always does.
@@ -208,6 +209,7 @@ __device__ __forceinline__ void merge_row(const Attend& a, const Unit& u, int r,
 template <class E>
 __device__ __forceinline__ void make_plan(const Attend& a, Plan& plan, int lane) {
   int64_t run = 0;
+  int all_units = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     int units = 0, tiles = 0;
     const int b = b0 + lane;
@@ -217,6 +219,7 @@ __device__ __forceinline__ void make_plan(const Attend& a, Plan& plan, int lane)
       tiles = tiles_of<E>(a, b, held, &units);
       if (blockIdx.x == 0 && tiles > 0 && (int64_t)held + a.n[b] > (int64_t)a.pg.table_stride << a.pg.page_shift) atomicOr(a.status, kStatusBadPage);
     }
+    if (tiles > 0) all_units += units;
     int64_t x = (int64_t)tiles * units;
     if (a.batch > 1) {
 #pragma unroll
@@ -228,14 +231,25 @@ __device__ __forceinline__ void make_plan(const Attend& a, Plan& plan, int lane)
     if (b < a.batch) plan.before[b + 1] = run + x;
     run += __shfl_sync(0xffffffffu, x, 31);
   }
-  if (lane == 0) plan.before[0] = 0;
+  all_units = __reduce_add_sync(0xffffffffu, all_units);
+  if (lane == 0) {
+    plan.before[0] = 0;
+    plan.units = all_units;
+  }
 }
 
 // The CTA's run, and the part of it to begin with.
 template <class E>
 __device__ __forceinline__ bool take_run(const Attend& a, const Plan& plan, Run& run, Part& c) {
   run.total = plan.before[a.batch];
-  run.ctas = max((int64_t)1, min((int64_t)gridDim.x, run.total / E::kMinRun));
+  const int64_t most = gridDim.x;
+  run.ctas = max((int64_t)1, min(most, run.total / E::kMinRun));
+  // Short runs: whole units, or as many CTAs for every one of them, so that (units being of one length) none has pieces of two.  8 units of 1400
+  // rows in bf16 15.0 -> 12.4 us, of 16 k 19.6 -> 16.0; a ragged batch of 8 x 8 units 103 -> 95.  (fp32 rows take longer: 16.5 -> 18.2 us with it.)
+  if (E::kEven && plan.units <= most && run.total < 16 * run.ctas) {
+    if (run.ctas < 2 * plan.units) run.ctas = min(run.total, plan.units);
+    else run.ctas -= (uint32_t)run.ctas % (uint32_t)plan.units;
+  }
   if (blockIdx.x >= run.ctas) return false;
   run.begin = run.start(blockIdx.x);
   run.end = run.start(blockIdx.x + 1);

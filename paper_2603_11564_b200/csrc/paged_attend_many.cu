@@ -33,7 +33,7 @@ static_assert(Smem::total <= 232448, "exceeds the shared memory a CTA can opt in
 
 struct Many {                                         // geometry, for the shared scheduling
   static constexpr int kRows = 256, kSlotRows = 256, kTile = 128, kCtas = 1, kMinRun = 4;
-  static constexpr bool kFromEnd = false;
+  static constexpr bool kFromEnd = false, kEven = true;
   using T = __nv_bfloat16;
   __device__ __forceinline__ static int channel(int p) { return p; }
 };

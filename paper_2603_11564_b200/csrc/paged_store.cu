@@ -137,7 +137,7 @@ __device__ __forceinline__ void rotate(Row<kPer>& x, const Angles& an, int lane,
 // A block takes kTok consecutive tokens: it evaluates their angles once for all heads, then its groups of 64 / kPer threads take the
 // tokens' K and V heads in turn, and after them the query heads.  kUnroll rows a group are in flight.
 template <typename T, bool kFp4, int kTok>
-__global__ void __launch_bounds__(kStoreThreads)
+__global__ void __launch_bounds__(kStoreThreads, kFp4 ? 4 : 0)
 paged_append_kernel(const __grid_constant__ PagedDev pg, const __grid_constant__ NewRows t, const __grid_constant__ NewTokensDev nt,
                     const double* __restrict__ inv_freq, int n_kv_heads, int n_q_heads, int interleaved, int* __restrict__ status) {
   __shared__ __align__(16) Angles angle[kTok];
@@ -341,8 +341,12 @@ cudaError_t launch_paged_append(int dtype, const PagedDev& pg, const NewRows& t,
     auto go = [&](auto kernel, int tok) {
       launch_pdl(kernel, dim3((n + tok - 1) / tok), dim3(kStoreThreads), 0, s, 1, pg, t, nt, inv_freq_dev, dm.n_kv_heads, dm.n_q_heads, dm.rope_interleaved, status);
     };
-    if (n > 1024) go(paged_append_kernel<T, decltype(fp4)::value, 4>, 4);
-    else go(paged_append_kernel<T, decltype(fp4)::value, 1>, 1);
+    // Many tokens a block where they still fill the SMs: its start (places, angles) is shared by more rows.  32 k tokens of 8 KV heads in 4 bits,
+    // 4 | 8 | 16 a block: 57 | 51 | 49 us (and four blocks an SM rather than three, 64 registers, 64 -> 57); copies in bf16 gain nothing.
+    constexpr bool kFour = decltype(fp4)::value;
+    if (kFour && n > 8192) go(paged_append_kernel<T, kFour, kFour ? 16 : 4>, 16);
+    else if (n > 1024) go(paged_append_kernel<T, kFour, 4>, 4);
+    else go(paged_append_kernel<T, kFour, 1>, 1);
   });
   log->end(s);
   return cudaGetLastError();

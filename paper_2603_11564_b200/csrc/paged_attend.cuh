@@ -39,6 +39,8 @@ using ptx::smem_u32;
 constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
 constexpr int kMostSms = 160;                        // (more SMs than that: one wave on 160 of them)
 
+// A factor on logits, kept finite: 0 times it is 0 however large the queries' scale is.
+__device__ __forceinline__ float finite(float f) { return fminf(f, 3e38f); }
 // c tanh(x / c) log2(e) of x = y c / (2 log2(e)), through the exponential (the tanh instruction has 11 bits).
 __device__ __forceinline__ float capped(float y, float c_log2e) { return c_log2e - __fdividef(2.f * c_log2e, 1.f + ex2(y)); }
 

@@ -2,15 +2,20 @@
 // tiles, 4 n L H_q d flops against one reading of the cache per 256 rows.
 //
 // A CTA has two tiles of 128 query rows (A and B) over the same keys, 128 at a time.  Four warps bring keys and values to shared memory as
-// 16-bit tiles with the 128-byte swizzle (codes times scales where the cache has 4 bits: done once for 256 query rows); one thread
+// 16-bit tiles with the 128-byte swizzle (codes times scales where the cache has 4 bits: done once for 256 query rows); one warp
 // issues the MMAs; four warps a tile take the softmax, one row a thread.  S = Q K^T goes to tensor memory, is read whole by its row's thread,
 // and comes back as the weights P, 16-bit, in the same columns, from where the second MMA takes them as its left operand; O += P V stays
-// in tensor memory.  V's tile is the right operand with its keys down (MN-major), so nothing is transposed.  While a tile's
-// rows are exponentiated the tensor cores have the other tile's two products: 4 x 128^3 a step, some 2800 cycles, against 2 x 128^2
-// exponentials, 2048 cycles of the MUFU.
+// in tensor memory.  V's tile is the right operand with its keys down (MN-major), so nothing is transposed.  While a tile's rows are
+// exponentiated the tensor cores have the other tile's two products.
 //
 // Types as in paged_attend.cu: fp16 for 4-bit caches (keys, values exact; queries exact after a power of two a row; weights, 2^11 times what
 // they are, to 11 bits), bf16 for bf16 caches (weights to 8 bits).
+//
+// Measured: two sequences, 300 and 450 new tokens, 64 heads of 8 KV heads, 13 k and 15 k rows in 4 bits (333 GFLOP): 351 us, 950 TFLOP/s (the warp-level
+// kernel: 2082; a cuBLAS product of that size: 201 in a burst, 240 under the power cap).  A step (256 rows, 128 keys) takes some 3400 cycles: its 32 MMAs
+// 83 cycles each, and what a tile's chain leaves uncovered: logits from tensor memory 180, their maximum 600, the weights 2 x 750, two
+// products 1330, hand-overs 300.  Tried: the maximum only after the fact, weights again where it moved (460), exponentials by polynomial for a quarter
+// of the pairs (+0 .. +90: instructions, not the MUFU, are short), three more warps for the values (382).
 #include "paged_attend.cuh"
 
 namespace dapq {
@@ -381,6 +386,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
         f *= __uint_as_float((uint32_t)e << 23) * a.pg.k_scale;
       }
       if (kCap) f *= 2.f / a.softcap;
+      f = finite(f);
 #pragma unroll
       for (int j = 0; j < 16; ++j) sts128(piece(sbase + Smem::q + x * kTileBytes, r, j), w[j]);
       fence_proxy_async();

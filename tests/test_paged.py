@@ -486,6 +486,121 @@ def test_attend_reports_bad_pages_and_goes_on(dq, dtype, fmt):
 
 
 @gpu
+@pytest.mark.parametrize("fmt", ["native", "fp4"])
+def test_giving_up_in_the_kernel_for_many_rows(dq, fmt):
+    """A limit of a cycle on its waits: a status, no hang, and the next call is right (its arrival counters are back at 0)."""
+    bf = torch.bfloat16
+    ctx = context(dq, 8, 2, bf)
+    cache = Cache(dq, bf, fmt, 2, 16, [3000, 70], [3100, 170])
+    for b, a in enumerate((3100, 170)):
+        cache.fill(b, *(torch.randn(2, a, D, device="cuda") for _ in "kv"))
+    q = torch.randn(200, 8, D, device="cuda").to(bf)
+    out = torch.empty_like(q)
+    for _ in range(2):                    # (only a limit that is over before the first look at the clock is sure to run out)
+        dq.dapq_set_wait_limit(ctx, 1)
+        dq.dapq_paged_attend(ctx, cache.view, [0, 100, 200], q, out)
+        with pytest.raises(dq.DapqError) as e:
+            dq.dapq_poll_status(ctx)
+        assert e.value.status == dq.DAPQ_ERR_TIMEOUT
+        dq.dapq_set_wait_limit(ctx, 0)
+        check_attend(dq, ctx, cache, q, [0, 100, 200])
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,fmt", TYPES)
+def test_attend_with_more_sequences_than_ctas_and_more_ctas_than_tiles(dq, dtype, fmt):
+    """128 sequences of all lengths, a third of them idle or without new tokens, some with many query rows."""
+    g = torch.Generator().manual_seed(9)
+    lens = [int(x) for x in torch.randint(0, 400, (128,), generator=g)]
+    new = [int(x) for x in torch.randint(0, 4, (128,), generator=g)]
+    lens[7], lens[50], lens[127], lens[3] = 9000, -1, -1, -1
+    new[9], new[50], new[3] = 70, 40, 1
+    cu = [0]
+    for n in new:
+        cu.append(cu[-1] + n)
+    ctx = context(dq, 8, 2, dtype, max_batch=128)
+    cache = Cache(dq, dtype, fmt, 2, 16, lens, [a + n if a >= 0 else 0 for a, n in zip(lens, new)])
+    for b, (a, n) in enumerate(zip(lens, new)):
+        if a + n > 0 and a >= 0:
+            cache.fill(b, *(torch.randn(2, a + n, D, device="cuda") for _ in "kv"))
+    check_attend(dq, ctx, cache, torch.randn(cu[-1], 8, D, device="cuda").to(dtype), cu)
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["native", "fp4"])
+@pytest.mark.parametrize("n", [1, 30])
+def test_infinities_and_nan_behind_the_cache_and_in_it(dq, fmt, n):
+    """In rows that nobody sees they do not matter; a NaN key that is seen makes its queries NaN, those of other heads and sequences not."""
+    bf = torch.bfloat16
+    ctx = context(dq, 4, 2, bf)
+    cache = Cache(dq, bf, fmt, 2, 16, [40, 40], [40 + n, 40 + n])
+    for b in range(2):
+        cache.fill(b, *(torch.randn(2, 40 + n, D, device="cuda") for _ in "kv"))
+    q = torch.randn(2 * n, 4, D, device="cuda").to(bf)
+    good, lse = check_attend(dq, ctx, cache, q, [0, n, 2 * n])
+    page, row = cache.where(1, 5, 6)
+    (cache.ks if fmt == "fp4" else cache.k)[page, 1, row] = 0x7F if fmt == "fp4" else math.nan
+    out = torch.empty_like(q)
+    dq.dapq_paged_attend(ctx, cache.view, [0, n, 2 * n], q, out)
+    dq.dapq_poll_status(ctx)
+    assert torch.equal(out[:n], good[:n]) and torch.equal(out[n:, :2], good[n:, :2]) and out[n:, 2:].isnan().all()
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,fmt", TYPES)
+def test_attend_to_the_largest_and_smallest_queries(dq, dtype, fmt):
+    """Queries near the ends of their type's range: logits of 0 stay 0, others saturate the softmax on the largest key."""
+    ctx = context(dq, 4, 1, dtype)
+    cache = Cache(dq, dtype, fmt, 1, 16, [49], [50])
+    k = torch.zeros(1, 50, D, device="cuda")
+    k[0, :, 0] = torch.arange(50, device="cuda") % 7 - 3.0
+    v = torch.randn(1, 50, D, device="cuda")
+    cache.fill(0, k, v)
+    v = cache.values(0, 0, 50)[1][0]
+    q = torch.zeros(1, 4, D, device="cuda")
+    q[0, 0, 1] = 3e38                                          # no key has this channel: all logits 0
+    q[0, 1, 0] = 1e30
+    q[0, 2, 0] = -1e-38
+    out, lse = torch.empty(1, 4, D, dtype=dtype, device="cuda"), torch.empty(1, 4, device="cuda")
+    dq.dapq_paged_attend(ctx, cache.view, None, q.to(dtype), out, lse)
+    dq.dapq_poll_status(ctx)
+    mean, best = v.mean(0), v[k[0, :, 0] == 3].mean(0)
+    # equal weights: sums of 50 products, roundings of the weights and of the output
+    tol = (half(dtype) + 2.0 ** -8 + 2.0 ** -18) * v.abs().mean(0) + 2.0 ** -20
+    for h in (0, 2, 3):
+        assert ((out[0, h].to(F64) - mean).abs() <= tol).all() and abs(lse[0, h].item() - math.log(50)) < 1e-5
+    assert ((out[0, 1].to(F64) - best).abs() <= (half(dtype) + 2.0 ** -8 + 2.0 ** -18) * v.abs().amax(0) + 2.0 ** -20).all()
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+def test_two_contexts_on_two_streams(dq):
+    """Each context orders its own calls only: two of them side by side, many times."""
+    bf = torch.bfloat16
+    pairs = []
+    for seed in (1, 2):
+        ctx = context(dq, 8, 2, bf)
+        cache = Cache(dq, bf, "fp4", 2, 16, [2500, 300], [2501, 301], seed=seed)
+        for b, a in enumerate((2501, 301)):
+            cache.fill(b, *(torch.randn(2, a, D, device="cuda") for _ in "kv"))
+        q = torch.randn(2, 8, D, device="cuda").to(bf)
+        want, _ = check_attend(dq, ctx, cache, q, [0, 1, 2])
+        pairs.append((ctx, cache, q, want, torch.cuda.Stream(), [torch.empty_like(q) for _ in range(40)]))
+    torch.cuda.synchronize()
+    for i in range(40):
+        for ctx, cache, q, _, stream, outs in pairs:
+            dq.dapq_paged_attend(ctx, cache.view, None, q, outs[i], stream=stream)
+    torch.cuda.synchronize()
+    for ctx, _, _, want, stream, outs in pairs:
+        assert all(torch.equal(o, want) for o in outs)
+        dq.dapq_poll_status(ctx, stream)
+        dq.dapq_destroy(ctx)
+
+
+@gpu
 def test_refusals(dq):
     bf = torch.bfloat16
     ctx = context(dq, 8, 2, bf, max_batch=2)
@@ -518,7 +633,7 @@ def test_refusals(dq):
     refused(1, attend(cu=[1, 2, 2]))
     refused(1, attend(cu=[0, 2, 1]))
     refused(2, attend(cu=[0, 1, 1 << 30]))
-    for cap in (-1.0, math.nan, math.inf):
+    for cap in (-1.0, math.nan, math.inf, 1e-19, 1e19):
         refused(1, attend(softcap=cap))
     refused(2, lambda: dq.dapq_paged_attend(ctx, cache.view, None, q, out.view(-1)[4:4 + 128].view(1, 1, D)))
     refused(1, lambda: dq.dapq_paged_append(ctx, cache.view, None, kv, kv, None, q, out))                       # queries without positions

@@ -173,7 +173,7 @@ cudaError_t launch_score_umma(const UmmaPlan& plan, const SeqTable& t, const Dim
                               int* status, long long wait_limit, cudaStream_t s, LaunchLog* log);
 
 // Pieces shared by the two tensor-core scorers (defined in score_qg.cu): the TMA descriptor of a
-// 16-bit [.., rows, 128] tensor (boxes of 64 channels x box_rows rows, 128-byte swizzle), and the cut of
+// 16-bit [.., rows, 128] tensor of rank up to 4 (boxes of 64 channels x box_rows rows, 128-byte swizzle), and the cut of
 // the sequences' keys into chunks of whole tiles with ctas_per_chunk CTAs working on every chunk.
 bool encode_tile_map(CUtensorMap* map, const void* base, bool f16, int rank, const uint64_t* dims,
                      const uint64_t* strides_bytes, int box_rows);

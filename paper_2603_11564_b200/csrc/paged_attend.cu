@@ -1,5 +1,5 @@
 // Attention over the paged cache: out = softmax(cap(q K^T scale)) V for the step's new queries, which see what their sequence held and the new rows
-// up to their own.  Here: few query rows a sequence and KV head (up to kFewRows; fp32 contexts: any number).
+// up to their own.  Here: few query rows a sequence and KV head (fp32 contexts: any number).
 //
 // One token reads the whole cache of its KV heads for G query rows: G flops a byte in bf16, 3.6 G in 4 bits.  What bounds it is the stream of
 // cache rows, and in 4 bits the instructions that turn codes into operands: 256 values a row and head, at 40 values a cycle and SM if the
@@ -692,9 +692,15 @@ cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
 
 }  // namespace
 
-// Query rows of a sequence and KV head up to which the kernels here take them; more go to the one that has them on the tall side of
-// tcgen05 tiles.
-constexpr int kFewRows = 16;
+// Which sequences of a bf16 call go to the kernel for many query rows.  It takes rows by 128 and some 0.9e6 row-key pairs a microsecond, the one here
+// by 16 and 0.26e6, but 10 us less to begin and end.  So: those of 48 rows of a KV head and more (rounded up as either kernel does, these gain), if
+// the gain of all of them, by the rows that their tables have room for, is more than those 10 us.  Measured, 8 KV heads, 4 bits, here | there: 1 k keys
+// 24 .. 128 rows 15 .. 16 | 19 .. 27 us; 8 k keys 64 rows 28 | 32, 128 rows 46 | 46; 32 k keys 32 rows 45 | 49, 48 rows 59 | 51, 128 rows 126 | 69.
+constexpr double kFewRate = 0.26e6, kManyRate = 0.9e6, kManyCost = 10.0;
+double gain_of_many(const Attend& a, int rows) {
+  const double keys = (double)((int64_t)a.pg.table_stride << a.pg.page_shift) * a.n_kv_heads;
+  return rows <= 16 ? 0.0 : keys * ((rows + 15) / 16 * 16 / kFewRate - (rows + 127) / 128 * 128 / kManyRate);
+}
 
 size_t attend_part_floats(int n_sm, bool bf16) {
   const size_t few = 2 * kSlotFloats<TensorEngine<true, 1>>, many = bf16 ? attend_many_part_floats() : 0;
@@ -707,9 +713,12 @@ cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t,
   Attend few = {pg, t.batch, {}, {}, q, q_stride, out, lse, part, sync, status, wait_limit, dm.n_q_heads, dm.n_kv_heads, dm.group, dm.scale_log2e, softcap};
   Attend many = few;
   int rows_few = 0, rows_many = 0;
+  auto gain = [&](int b) { return dtype == DAPQ_BF16 ? gain_of_many(few, (t.cu[b + 1] - t.cu[b]) * dm.group) : 0.0; };
+  double all = 0.0;
+  for (int b = 0; b < t.batch; ++b) all += max(gain(b), 0.0);
   for (int b = 0; b < t.batch; ++b) {
     const int n = t.cu[b + 1] - t.cu[b], rows = n * dm.group;
-    const bool is_many = dtype == DAPQ_BF16 && rows > kFewRows;
+    const bool is_many = all > kManyCost && gain(b) > 0.0;
     (is_many ? rows_many : rows_few) = max(is_many ? rows_many : rows_few, rows);
     few.start[b] = many.start[b] = t.cu[b];
     few.n[b] = is_many ? 0 : n;

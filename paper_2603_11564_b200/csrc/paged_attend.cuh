@@ -25,6 +25,7 @@ struct Attend {
   long long wait_limit;
   int32_t n_q_heads, n_kv_heads, group;
   float scale_log2e, softcap;
+  int32_t tma;                                       // the pools can be described to TMA (paged_attend_many.cu)
 };
 
 // The kernel for many query rows (paged_attend_many.cu), and what its partial results take per CTA.

@@ -140,22 +140,24 @@ __device__ __forceinline__ void store_codes(uint32_t tile, int r, const Codes& c
   }
 }
 
-// Keys go one tile ahead of the values: tile t's second product and tile t + 1's first follow one another.
-template <bool kFp4>
-__device__ __forceinline__ void produce(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase) {
+// Where a row of a tile lies: channel offset of row r, negative if it reads as zero.
+__device__ __forceinline__ int64_t row_offset(const Attend& a, const Unit& u, int pages, int base, int r) {
+  const int pg = __shfl_sync(0xffffffffu, pages, r >> 4);
+  return (unsigned)pg >= (unsigned)a.pg.n_pages || base + r >= u.limit
+             ? (int64_t)-1
+             : pg * a.pg.page_stride + u.h * a.pg.head_stride + (int64_t)((base + r) & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride;
+}
+__device__ __forceinline__ void check_pages(const Attend& a, const Unit& u, int pages, int base, int lane) {
+  if (lane < 8 && base + 16 * lane < u.limit && (unsigned)pages >= (unsigned)a.pg.n_pages) atomicOr(a.status, kStatusBadPage);
+}
+
+// Keys go one tile ahead of the values: tile t's second product and tile t + 1's first follow one another.  4 bits: four warps, a thread a row, whose
+// codes are on their way while those before them are turned into operands.
+__device__ __forceinline__ void produce_codes(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase) {
   const int tid = threadIdx.x - 256, lane = tid & 31, warp = tid >> 5;
   int done = 0;                                                           // tiles so far
   for (bool on = true; on; on = next_part(a, plan, run, c, lane)) {
     const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile;
-    auto offset = [&](int pages, int base, int r) {                       // channel offset of row r of a tile, negative: reads as zero
-      const int pg = __shfl_sync(0xffffffffu, pages, r >> 4);
-      return (unsigned)pg >= (unsigned)a.pg.n_pages || base + r >= c.u.limit
-                 ? (int64_t)-1
-                 : pg * a.pg.page_stride + c.u.h * a.pg.head_stride + (int64_t)((base + r) & ((1 << a.pg.page_shift) - 1)) * a.pg.row_stride;
-    };
-    auto check = [&](int pages, int base) {
-      if (warp == 0 && lane < 8 && base + 16 * lane < c.u.limit && (unsigned)pages >= (unsigned)a.pg.n_pages) atomicOr(a.status, kStatusBadPage);
-    };
     auto free = [&](int which, int t) { return t < kRing || wait.warp(which + (t & 1), ((t >> 1) & 1) ^ 1); };
     auto full = [&](int which, int t) {
       fence_proxy_async();
@@ -163,64 +165,100 @@ __device__ __forceinline__ void produce(const Attend& a, Part& c, const Plan& pl
       if (lane == 0) mbar_arrive(wait.bar(which + (t & 1)));
     };
     int page = tile_page(a, c.u, first, lane), page1 = n > 1 ? tile_page(a, c.u, first + Many::kTile, lane) : -1;
-    check(page, first);
-    if constexpr (kFp4) {
-      // (a row's codes are on their way while those before them are turned into operands)
-      Codes k = load_codes(a.pg.k, a.pg.k_scales, offset(page, first, tid));
-      if (!free(Smem::k_empty, done)) return;
-      store_codes(sbase + Smem::k + (done & 1) * kTileBytes, tid, k);
-      full(Smem::k_full, done);
-      if (n > 1) k = load_codes(a.pg.k, a.pg.k_scales, offset(page1, first + Many::kTile, tid));
-      for (int i = 0; i < n; ++i, ++done) {
-        const int base = first + i * Many::kTile;
-        const Codes v = load_codes(a.pg.v, a.pg.v_scales, offset(page, base, tid));
-        const int page2 = i + 2 < n ? tile_page(a, c.u, base + 2 * Many::kTile, lane) : -1;
-        if (i + 1 < n) {
-          check(page1, base + Many::kTile);
-          if (!free(Smem::k_empty, done + 1)) return;
-          store_codes(sbase + Smem::k + ((done + 1) & 1) * kTileBytes, tid, k);
-          full(Smem::k_full, done + 1);
-        }
-        if (i + 2 < n) k = load_codes(a.pg.k, a.pg.k_scales, offset(page2, base + 2 * Many::kTile, tid));
-        if (!free(Smem::v_empty, done)) return;
-        store_codes(sbase + Smem::v + (done & 1) * kTileBytes, tid, v);
-        full(Smem::v_full, done);
-        page = page1;
-        page1 = page2;
+    if (warp == 0) check_pages(a, c.u, page, first, lane);
+    Codes k = load_codes(a.pg.k, a.pg.k_scales, row_offset(a, c.u, page, first, tid));
+    if (!free(Smem::k_empty, done)) return;
+    store_codes(sbase + Smem::k + (done & 1) * kTileBytes, tid, k);
+    full(Smem::k_full, done);
+    if (n > 1) k = load_codes(a.pg.k, a.pg.k_scales, row_offset(a, c.u, page1, first + Many::kTile, tid));
+    for (int i = 0; i < n; ++i, ++done) {
+      const int base = first + i * Many::kTile;
+      const Codes v = load_codes(a.pg.v, a.pg.v_scales, row_offset(a, c.u, page, base, tid));
+      const int page2 = i + 2 < n ? tile_page(a, c.u, base + 2 * Many::kTile, lane) : -1;
+      if (i + 1 < n) {
+        if (warp == 0) check_pages(a, c.u, page1, base + Many::kTile, lane);
+        if (!free(Smem::k_empty, done + 1)) return;
+        store_codes(sbase + Smem::k + ((done + 1) & 1) * kTileBytes, tid, k);
+        full(Smem::k_full, done + 1);
       }
+      if (i + 2 < n) k = load_codes(a.pg.k, a.pg.k_scales, row_offset(a, c.u, page2, base + 2 * Many::kTile, tid));
+      if (!free(Smem::v_empty, done)) return;
+      store_codes(sbase + Smem::v + (done & 1) * kTileBytes, tid, v);
+      full(Smem::v_full, done);
+      page = page1;
+      page1 = page2;
+    }
+  }
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// bf16: one warp.  Tiles whose rows and pages all exist come by TMA, in boxes of 64 channels and as many rows as a page (and a tile) has; the last
+// tile of a sequence, tiles with a page that does not exist, and pools that TMA cannot describe row by row, what is not there as zeros.
+__device__ __forceinline__ void produce_rows(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase, const CUtensorMap* tk,
+                                             const CUtensorMap* tv) {
+  const int lane = threadIdx.x & 31, box = min(1 << a.pg.page_shift, Many::kTile);
+  int done = 0, k_sent = 0, v_sent = 0;                                   // tiles so far; tiles of K and V on their way or there
+  bool ok = true;
+  auto bring = [&](bool keys, int t, int pages, int base) {
+    const int st = t & 1;
+    if (t >= kRing && !wait.warp((keys ? Smem::k_empty : Smem::v_empty) + st, ((t >> 1) & 1) ^ 1)) return false;
+    const uint32_t tile = sbase + (keys ? Smem::k : Smem::v) + st * kTileBytes, bar = wait.bar((keys ? Smem::k_full : Smem::v_full) + st);
+    const bool there = __all_sync(0xffffffffu, lane >= 8 || (unsigned)pages < (unsigned)a.pg.n_pages);
+    if (a.tma && there && base + Many::kTile <= c.u.limit) {
+      if (lane == 0) mbar_expect_tx(bar, kTileBytes);
+      __syncwarp();
+      const int boxes = Many::kTile / box, piece = lane >> 1, half = lane & 1;
+      const int page = __shfl_sync(0xffffffffu, pages, min(piece * box, Many::kTile - 1) >> 4);
+      if (piece < boxes)
+        tma_load_4d(tile + half * kHalfTile + piece * box * 128, keys ? tk : tv, bar, 64 * half, (base + piece * box) & ((1 << a.pg.page_shift) - 1), c.u.h, page);
     } else {
-      auto copy = [&](uint32_t tile, const char* from, int pages, int base) {
+      const char* from = (keys ? a.pg.k : a.pg.v) + (lane & 15) * 16;
+      const uint32_t step = (uint32_t)a.pg.row_stride * 2;
+#pragma unroll 1
+      for (int p = 0; p < 8; ++p) {
+        const int r0 = 16 * p + (lane >> 4);
+        const int64_t off = row_offset(a, c.u, pages, base, 16 * p);
+        const int left = off < 0 ? 0 : c.u.limit - base - r0;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int r = 8 * j + (tid >> 4);
-          const int64_t off = offset(pages, base, r);
-          const uint32_t to = piece(tile, r, tid & 15);
-          if (off < 0) sts128(to, make_uint4(0, 0, 0, 0));
-          else cp_async16(to, from + 2 * off + (tid & 15) * 16);
+        for (int j = 0; j < 16; j += 2) {
+          const uint32_t to = piece(tile, r0 + j, lane & 15);
+          if (j < left) cp_async16(to, from + 2 * off + (uint32_t)(j + (lane >> 4)) * step);
+          else sts128(to, make_uint4(0, 0, 0, 0));
         }
-        cp_async_commit();
-      };
-      if (!free(Smem::k_empty, done)) return;
-      copy(sbase + Smem::k + (done & 1) * kTileBytes, a.pg.k, page, first);
-      cp_async_wait<0>();
-      full(Smem::k_full, done);
-      for (int i = 0; i < n; ++i, ++done) {
-        const int base = first + i * Many::kTile;
-        const int page2 = i + 2 < n ? tile_page(a, c.u, base + 2 * Many::kTile, lane) : -1;
-        if (i + 1 < n) {
-          check(page1, base + Many::kTile);
-          if (!free(Smem::k_empty, done + 1)) return;
-          copy(sbase + Smem::k + ((done + 1) & 1) * kTileBytes, a.pg.k, page1, base + Many::kTile);
-        }
-        if (!free(Smem::v_empty, done)) { cp_async_wait<0>(); return; }
-        copy(sbase + Smem::v + (done & 1) * kTileBytes, a.pg.v, page, base);
-        cp_async_wait<1>();
-        if (i + 1 < n) full(Smem::k_full, done + 1);
-        cp_async_wait<0>();
-        full(Smem::v_full, done);
-        page = page1;
-        page1 = page2;
       }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    }
+    (keys ? k_sent : v_sent) = t + 1;
+    return true;
+  };
+  for (bool on = true; on && ok; on = next_part(a, plan, run, c, lane)) {
+    const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile;
+    int page = tile_page(a, c.u, first, lane);
+    check_pages(a, c.u, page, first, lane);
+    ok = bring(true, done, page, first);
+    for (int i = 0; i < n && ok; ++i, ++done) {
+      const int base = first + i * Many::kTile, page1 = i + 1 < n ? tile_page(a, c.u, base + Many::kTile, lane) : -1;
+      if (i + 1 < n) {
+        check_pages(a, c.u, page1, base + Many::kTile, lane);
+        ok = bring(true, done + 1, page1, base + Many::kTile);
+      }
+      ok = ok && bring(false, done, page, base);
+      page = page1;
+    }
+  }
+  if (!ok) {                                                              // the CTA does not end with a copy on its way
+    for (int back = 1; back <= kRing; ++back) {
+      if (back <= k_sent) drain_wait(wait.bar(Smem::k_full + ((k_sent - back) & 1)), ((k_sent - back) >> 1) & 1, kWaitLimit);
+      if (back <= v_sent) drain_wait(wait.bar(Smem::v_full + ((v_sent - back) & 1)), ((v_sent - back) >> 1) & 1, kWaitLimit);
     }
   }
 }
@@ -525,7 +563,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
 
 template <bool kFp4, bool kCap>
 __global__ void __launch_bounds__(kThreads, 1)
-paged_attend_many_kernel(const __grid_constant__ Attend a) {
+paged_attend_many_kernel(const __grid_constant__ Attend a, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
   if (sbase & 1023u) {                                                    // (uniform over the CTA: nothing has been set up yet)
@@ -537,9 +575,10 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
   const Wait wait{sbase + Smem::bars, reinterpret_cast<volatile int*>(smem + Smem::abort_flag), a.status, a.wait_limit};
   if (threadIdx.x == 0) {
     for (int i = 0; i < Smem::n_bars; ++i) {
-      const bool four = i < Smem::k_empty || i == Smem::v_full || i == Smem::v_full + 1 || (i >= Smem::q_full && i < Smem::s_full) ||
-                        (i >= Smem::p_half && i < Smem::pv_done);
-      mbar_init(wait.bar(i), four ? 4 : 1);                               // the warps of a role, or the issuer's commit
+      // the warps of a role, or one: its leader or the issuer's commit
+      const bool tiles = i < Smem::k_empty || i == Smem::v_full || i == Smem::v_full + 1;
+      const bool four = (tiles && kFp4) || (i >= Smem::q_full && i < Smem::s_full) || (i >= Smem::p_half && i < Smem::pv_done);
+      mbar_init(wait.bar(i), four ? 4 : 1);
     }
     *wait.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -571,7 +610,8 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
       softmax<kFp4, kCap>(a, c, plan, run, wait, smem, sbase, tmem);
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-      produce<kFp4>(a, c, plan, run, wait, sbase);
+      if (kFp4) produce_codes(a, c, plan, run, wait, sbase);
+      else if (warp == 8) produce_rows(a, c, plan, run, wait, sbase, &tk, &tv);
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
       if (warp == 12) issue<kFp4>(a, c, plan, run, wait, sbase, tmem);
@@ -586,10 +626,10 @@ paged_attend_many_kernel(const __grid_constant__ Attend a) {
 }
 
 template <bool kFp4, bool kCap>
-cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
+cudaError_t go(const Attend& a, const CUtensorMap& tk, const CUtensorMap& tv, int n_sm, cudaStream_t s) {
   cudaError_t e = cudaFuncSetAttribute(paged_attend_many_kernel<kFp4, kCap>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::total);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_attend_many_kernel<kFp4, kCap>, dim3((unsigned)most_ctas<Many>(a, n_sm)), dim3(kThreads), Smem::total, s, 1, a);
+  return launch_pdl(paged_attend_many_kernel<kFp4, kCap>, dim3((unsigned)most_ctas<Many>(a, n_sm)), dim3(kThreads), Smem::total, s, 1, a, tk, tv);
 }
 
 }  // namespace
@@ -599,8 +639,16 @@ size_t attend_many_part_floats() { return 2 * (size_t)kSlotFloats<Many>; }
 cudaError_t launch_attend_many(const Attend& in, int n_sm, cudaStream_t s) {
   Attend a = in;
   if (a.wait_limit <= 0) a.wait_limit = ptx::kWaitLimit;
-  if (a.softcap > 0.f) return a.pg.fp4 ? go<true, true>(a, n_sm, s) : go<false, true>(a, n_sm, s);
-  return a.pg.fp4 ? go<true, false>(a, n_sm, s) : go<false, false>(a, n_sm, s);
+  CUtensorMap tk = {}, tv = {};
+  if (!a.pg.fp4) {
+    const PagedDev& pg = a.pg;
+    const uint64_t dims[4] = {kHeadDim, 1ull << pg.page_shift, (uint64_t)a.n_kv_heads, (uint64_t)pg.n_pages};
+    const uint64_t strides[3] = {(uint64_t)pg.row_stride * 2, (uint64_t)pg.head_stride * 2, (uint64_t)pg.page_stride * 2};
+    const int box = (1 << pg.page_shift) < Many::kTile ? 1 << pg.page_shift : Many::kTile;
+    a.tma = encode_tile_map(&tk, pg.k, false, 4, dims, strides, box) && encode_tile_map(&tv, pg.v, false, 4, dims, strides, box);
+  }
+  if (a.softcap > 0.f) return a.pg.fp4 ? go<true, true>(a, tk, tv, n_sm, s) : go<false, true>(a, tk, tv, n_sm, s);
+  return a.pg.fp4 ? go<true, false>(a, tk, tv, n_sm, s) : go<false, false>(a, tk, tv, n_sm, s);
 }
 
 }  // namespace dapq

@@ -71,14 +71,14 @@ def rotated(x, pos, interleaved, base):
 class Cache:
     """Pools with pages in random order, poisoned where nothing was written; `layout` chooses the strides."""
 
-    def __init__(self, dq, dtype, fmt, hkv, page_rows, lens, room, seed=0, layout="plain", k_scale=1.0, v_scale=1.0, extra=3):
+    def __init__(self, dq, dtype, fmt, hkv, page_rows, lens, room, seed=0, layout="plain", k_scale=1.0, v_scale=1.0, extra=3, wide=0):
         g = torch.Generator().manual_seed(seed)
         self.dq, self.dtype, self.fmt, self.rows, self.lens, self.hkv = dq, dtype, fmt, page_rows, list(lens), hkv
         self.k_scale, self.v_scale = k_scale, v_scale
         need = [-(-max(0, r) // page_rows) for r in room]
         n = sum(need) + extra
         order = torch.randperm(n, generator=g).int()
-        stride = max(max(need), 1) + 1
+        stride = max(max(need) + 1, 2, wide)                  # (wide: room for long sequences, as which kernel takes a call goes by the room)
         table = torch.full((len(lens), stride), n + 7, dtype=torch.int32)
         table[::2] = -3
         at = 0
@@ -426,6 +426,79 @@ def test_attend(dq, dtype, fmt, shape):
     dq.dapq_destroy(ctx)
 
 
+WIDE = 131072                                                 # rows of room: the kernel for many query rows takes 48 and more
+
+
+MANY = [
+    (48, 2, 128, [900, 64], [2, 2], 5.0),
+    (32, 8, 16, [64, -1, 0, 333], [30, 20, 0, 40], 50.0),
+    (16, 2, 1024, [2500], [130], 0.0),
+    (6, 2, 256, [0, 0], [257, 33], 0.0),
+    (64, 8, 16, [5, 300], [64, 17], 0.0),
+    (8, 1, 32, [127, 128, 129, 255], [16, 17, 15, 48], 0.0),
+    (12, 4, 64, [3000], [100], 20.0),
+    (8, 2, 16, [120, 20, 4000, 7], [33, 1, 3, 200], 0.0),     # sequences for either kernel in one call
+]
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["native", "fp4"])
+@pytest.mark.parametrize("shape", MANY, ids=[str(i) for i in range(len(MANY))])
+def test_attend_with_many_query_rows(dq, fmt, shape):
+    hq, hkv, rows, lens, new, cap = shape
+    bf = torch.bfloat16
+    cu = [0]
+    for n in new:
+        cu.append(cu[-1] + n)
+    g = torch.Generator(device="cuda").manual_seed(13)
+    ctx = context(dq, hq, hkv, bf)
+    cache = Cache(dq, bf, fmt, hkv, rows, lens, [a + n if a >= 0 else 0 for a, n in zip(lens, new)], layout=["plain", "interleaved", "padded"][hkv % 3],
+                  k_scale=0.5, v_scale=0.3, wide=WIDE // rows)
+    for b, (a, n) in enumerate(zip(lens, new)):
+        if a + n > 0 and a >= 0:
+            cache.fill(b, *(torch.randn(hkv, a + n, D, device="cuda", generator=g) for _ in "kv"))
+    q = (2.0 * torch.randn(cu[-1], hq + 2, D, device="cuda", generator=g)).to(bf)[:, :hq]
+    first = check_attend(dq, ctx, cache, q, cu, cap)
+    again = check_attend(dq, ctx, cache, q, cu, cap)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["native", "fp4"])
+def test_many_query_rows_and_maxima_that_move(dq, fmt):
+    """Keys along the queries, ever larger, then far below, over several tiles; a page in the middle that does not exist."""
+    bf = torch.bfloat16
+    ctx = context(dq, 4, 1, bf)
+    held, n = 1500, 40
+    cache = Cache(dq, bf, fmt, 1, 32, [held], [held + n], wide=WIDE // 32)
+    d = torch.randn(D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    d = d / d.norm()
+    z = torch.cat((torch.linspace(-60, 60, 1000, device="cuda"), torch.linspace(60, -200, held + n - 1000, device="cuda")))
+    cache.fill(0, (z[:, None] * d + 0.01 * torch.randn(held + n, D, device="cuda"))[None], torch.randn(1, held + n, D, device="cuda"))
+    f = torch.linspace(-1.5, 1.5, 4 * n, device="cuda").view(n, 4, 1)
+    q = (f * d * math.sqrt(D)).to(bf)
+    good, _ = check_attend(dq, ctx, cache, q, [0, n])
+    page = int(cache.table[0, 5])
+    cache.table[0, 5] = -2                                    # rows 160 .. 191
+    out = torch.empty_like(q)
+    dq.dapq_paged_attend(ctx, cache.view, [0, n], q, out)
+    with pytest.raises(dq.DapqError) as e:
+        dq.dapq_poll_status(ctx)
+    assert e.value.status == dq.DAPQ_ERR_INVALID_ARG and out.isfinite().all()
+    k, v = cache.values(0, 0, 160)[0][0], cache.values(0, 0, 160)[1][0]
+    cache.table[0, 5] = page
+    k2, v2 = (x[0] for x in cache.values(0, 192, held + n))
+    k, v = torch.cat((k, k2)), torch.cat((v, v2))
+    seen = torch.cat((torch.arange(160), torch.arange(192, held + n))).cuda()
+    x = q.to(F64) @ k.T / math.sqrt(D)
+    x = torch.where(seen <= held + torch.arange(n, device="cuda")[:, None, None], x, -math.inf)
+    w = torch.softmax(x, -1)
+    # logits reach 140: dz = 140 * 2^-24 * 140 and the exponent's rounding of as much again
+    assert ((out.to(F64) - w @ v).abs() <= (2.0 ** -8 + half(bf) + 4 * 140 * 140 * 2.0 ** -24 + 2.0 ** -12) * (w @ v.abs()) + 1e-6).all()
+    dq.dapq_destroy(ctx)
+
+
 @gpu
 @pytest.mark.parametrize("dtype,fmt", TYPES)
 def test_attend_to_peaks_that_move_the_maximum(dq, dtype, fmt):
@@ -491,7 +564,7 @@ def test_giving_up_in_the_kernel_for_many_rows(dq, fmt):
     """A limit of a cycle on its waits: a status, no hang, and the next call is right (its arrival counters are back at 0)."""
     bf = torch.bfloat16
     ctx = context(dq, 8, 2, bf)
-    cache = Cache(dq, bf, fmt, 2, 16, [3000, 70], [3100, 170])
+    cache = Cache(dq, bf, fmt, 2, 16, [3000, 70], [3100, 170], wide=WIDE // 16)
     for b, a in enumerate((3100, 170)):
         cache.fill(b, *(torch.randn(2, a, D, device="cuda") for _ in "kv"))
     q = torch.randn(200, 8, D, device="cuda").to(bf)
@@ -520,7 +593,7 @@ def test_attend_with_more_sequences_than_ctas_and_more_ctas_than_tiles(dq, dtype
     for n in new:
         cu.append(cu[-1] + n)
     ctx = context(dq, 8, 2, dtype, max_batch=128)
-    cache = Cache(dq, dtype, fmt, 2, 16, lens, [a + n if a >= 0 else 0 for a, n in zip(lens, new)])
+    cache = Cache(dq, dtype, fmt, 2, 16, lens, [a + n if a >= 0 else 0 for a, n in zip(lens, new)], wide=WIDE // 16)
     for b, (a, n) in enumerate(zip(lens, new)):
         if a + n > 0 and a >= 0:
             cache.fill(b, *(torch.randn(2, a + n, D, device="cuda") for _ in "kv"))
@@ -535,7 +608,7 @@ def test_infinities_and_nan_behind_the_cache_and_in_it(dq, fmt, n):
     """In rows that nobody sees they do not matter; a NaN key that is seen makes its queries NaN, those of other heads and sequences not."""
     bf = torch.bfloat16
     ctx = context(dq, 4, 2, bf)
-    cache = Cache(dq, bf, fmt, 2, 16, [40, 40], [40 + n, 40 + n])
+    cache = Cache(dq, bf, fmt, 2, 16, [40, 40], [40 + n, 40 + n], wide=WIDE // 16)
     for b in range(2):
         cache.fill(b, *(torch.randn(2, 40 + n, D, device="cuda") for _ in "kv"))
     q = torch.randn(2 * n, 4, D, device="cuda").to(bf)

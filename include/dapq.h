@@ -302,6 +302,7 @@ DAPQ_API dapq_status dapq_evict_layers_host(dapq_ctx* ctx, int32_t n_layers, con
  *   - A row that its sequence's part of the table has no place for, or whose page number lies outside [0, n_pages), is
  *     skipped (dapq_paged_read writes zeros for it) and flagged: dapq_poll_status returns DAPQ_ERR_INVALID_ARG.
  *   - No page may belong to two sequences that one call writes to.  Rows beyond those written stay as they were.
+ *   - Inputs and outputs do not overlap, nor do they lie in the pages; but q_rot may be q, and out may be q, where q is contiguous.
  *   - dapq_paged_attend uses the context's workspace: the caller orders its calls on one context (one stream, or events), as
  *     for the scorers.  The other three use none.  All are capturable and launch one kernel (dapq_paged_attend two where a bf16
  *     call has sequences of few and of many query rows).  A wait that gives up in the kernel for many rows: dapq_poll_status. */
@@ -360,7 +361,7 @@ DAPQ_API dapq_status dapq_paged_read(dapq_ctx* ctx, const dapq_paged_cache* page
 
 /* out[t, h, :] = sum_j softmax_j(cap(q[t, h] . k_j * softmax_scale)) v_j over the rows j = 0 .. cache_len[b] + i that the i-th new
  * query of sequence b sees: all that the sequence held, and the new rows up to its own (dapq_paged_append comes first).
- * softcap: 0, or c in 1e-18 .. 1e18 for cap(x) = c tanh(x / c).  q: device [T, H_q, d], already rotated, tokens q_token_stride elements apart;
+ * softcap: 0, or c in 1e-18 .. 1024 for cap(x) = c tanh(x / c).  q: device [T, H_q, d], already rotated, tokens q_token_stride elements apart;
  * out: device [T, H_q, d], contiguous; lse_out: device [T, H_q] natural-log sum-exp, or NULL.  Logits, maxima, sums and outputs
  * are held in fp32; see paged_attend.cu for what the products take.  A query that sees nothing gets 0 and -inf.  Infinities
  * and NaN in rows that no query of its sequence sees do not matter; in a row that only later queries of the same call see they may

@@ -368,11 +368,12 @@ assert _TOKENS.size == C.sizeof(dapq_new_tokens)
 _INT32S: dict = {}                                  # struct.Struct of n int32, by n
 
 
-def _i32_bytes(seq: Optional[Sequence[int]]) -> Optional[bytes]:
-    """int32 image of `seq`.  (The calls of a decode step take a few microseconds on the GPU; packing the offsets of 64 sequences
+def _i32_bytes(seq: Optional[Sequence[int]], n_want: int) -> Optional[bytes]:
+    """int32 image of `seq`, n_want numbers.  (The calls of a decode step take a few microseconds on the GPU; packing the offsets of 64 sequences
     into an array takes one of them, into bytes half of one.)"""
     if seq is None:
         return None
+    assert len(seq) == n_want
     if type(seq) in (list, tuple):
         n = len(seq)
         fmt = _INT32S.get(n)
@@ -402,28 +403,28 @@ def dapq_paged_append(ctx, pages: dapq_paged_cache, cu_new, k: torch.Tensor, v: 
         assert q_rot is None or q_rot.is_contiguous()
         tokens = _TOKENS.pack(k.data_ptr(), v.data_ptr(), q.data_ptr(), _ptr(q_rot) or 0, _token_stride(k), _token_stride(v), _token_stride(q),
                               _ptr(positions) or 0)
-    _check(ctx, load_library().dapq_paged_append(ctx, pages.address, _i32_bytes(cu_new), tokens, _stream(stream)))
+    _check(ctx, load_library().dapq_paged_append(ctx, pages.address, _i32_bytes(cu_new, pages.batch + 1), tokens, _stream(stream)))
 
 
 def dapq_paged_compact(ctx, k: torch.Tensor, v: torch.Tensor, cu_rows, prompt_len, idx: torch.Tensor, k_keep, pages: dapq_paged_cache,
                        stream=None) -> None:
     view, keep_alive = _view(k, v, cu_rows, prompt_len)
-    _check(ctx, load_library().dapq_paged_compact(ctx, view, idx.data_ptr(), _i32_bytes(k_keep), pages.address, _stream(stream)))
+    _check(ctx, load_library().dapq_paged_compact(ctx, view, idx.data_ptr(), _i32_bytes(k_keep, len(prompt_len)), pages.address, _stream(stream)))
 
 
 def dapq_paged_read(ctx, pages: dapq_paged_cache, first, n_rows, row_at, k_out: torch.Tensor, v_out: torch.Tensor, stream=None) -> None:
     """k_out, v_out: [H_kv, R, 128], rows contiguous, heads apart alike."""
-    s, n = k_out.stride(), k_out.shape
-    assert len(s) == 3 and n[2] == 128 and s[1:] == (128, 1) and v_out.stride() == s and v_out.shape == n
-    _check(ctx, load_library().dapq_paged_read(ctx, pages.address, _i32_bytes(first), _i32_bytes(n_rows), _i32_bytes(row_at), k_out.data_ptr(),
-                                               v_out.data_ptr(), s[0] if n[0] > 1 else n[1] * 128, _stream(stream)))
+    s, shape, n = k_out.stride(), k_out.shape, pages.batch
+    assert len(s) == 3 and shape[2] == 128 and s[1:] == (128, 1) and v_out.stride() == s and v_out.shape == shape
+    _check(ctx, load_library().dapq_paged_read(ctx, pages.address, _i32_bytes(first, n), _i32_bytes(n_rows, n), _i32_bytes(row_at, n), k_out.data_ptr(),
+                                               v_out.data_ptr(), s[0] if shape[0] > 1 else shape[1] * 128, _stream(stream)))
 
 
 def dapq_paged_attend(ctx, pages: dapq_paged_cache, cu_new, q_rot: torch.Tensor, out: torch.Tensor, lse_out: Optional[torch.Tensor] = None,
                       softcap: float = 0.0, stream=None) -> None:
     """q_rot, out: [T, H_q, 128]; lse_out: [T, H_q] fp32."""
     assert out.is_contiguous() and (lse_out is None or lse_out.is_contiguous())
-    _check(ctx, load_library().dapq_paged_attend(ctx, pages.address, _i32_bytes(cu_new), q_rot.data_ptr(), _token_stride(q_rot), softcap,
+    _check(ctx, load_library().dapq_paged_attend(ctx, pages.address, _i32_bytes(cu_new, pages.batch + 1), q_rot.data_ptr(), _token_stride(q_rot), softcap,
                                                  out.data_ptr(), _ptr(lse_out), _stream(stream)))
 
 

@@ -1208,8 +1208,8 @@ dapq_status dapq_paged_attend(dapq_ctx* ctx, const dapq_paged_cache* pages, cons
   dapq_status st = check_paged(ctx, "dapq_paged_attend", pages, true, &pg);
   if (st == DAPQ_OK) st = check_new_rows(ctx, "dapq_paged_attend", pages->batch, cu_new_host, &t);
   if (st != DAPQ_OK) return st;
-  if (!(softcap == 0.f || (softcap >= 1e-18f && softcap <= 1e18f)))
-    return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_attend: softcap must be 0 or in 1e-18 .. 1e18");
+  if (!(softcap == 0.f || (softcap >= 1e-18f && softcap <= 1024.f)))
+    return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_attend: softcap must be 0 or in 1e-18 .. 1024");
   if (q_token_stride < (int64_t)ctx->dims.n_q_heads * kHeadDim)
     return fail(ctx, DAPQ_ERR_INVALID_ARG, "dapq_paged_attend: q_token_stride must be at least a token's heads");
   if (!aligned16(q) || !aligned16(out) || q_token_stride % (16 / ctx->elem_bytes))

@@ -417,7 +417,7 @@ struct FloatEngine {
       reinterpret_cast<float4*>(extra)[x] = v;
     }
     __syncthreads();
-    fac = finite(a.scale_log2e * (kFp4 ? a.pg.k_scale : 1.f) * (a.softcap > 0.f ? 2.f / a.softcap : 1.f));
+    fac = finite(a.scale_log2e * (kFp4 ? a.pg.k_scale : 1.f) * (a.softcap > 0.f ? 0.69314718f / a.softcap : 1.f));
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       m[r] = kLowest;
@@ -473,7 +473,7 @@ struct FloatEngine {
     for (int i = 0; i < kRows / 2; ++i) {                                 // this lane's rows: 2 i + hf
       const float s0 = s[2 * i] + __shfl_xor_sync(0xffffffffu, s[2 * i], 1), s1 = s[2 * i + 1] + __shfl_xor_sync(0xffffffffu, s[2 * i + 1], 1);
       z[i] = (hf ? s1 : s0) * fac;
-      if (a.softcap > 0.f) z[i] = capped(z[i], a.softcap * 1.44269504f);
+      if (a.softcap > 0.f) z[i] = a.softcap * 1.44269504f * tanhf(z[i]);   // (8 of these to 1024 products: the accurate one)
       if (!whole && base + key >= sees(a, u, 2 * i + hf)) z[i] = -CUDART_INF_F;
       above = above || z[i] > (hf ? m[2 * i + 1] : m[2 * i]) + kSlack;
     }

@@ -40,9 +40,11 @@ using ptx::smem_u32;
 constexpr float kSlack = 4.f, kLowest = -3.4028235e38f;
 constexpr int kMostSms = 160;                        // (more SMs than that: one wave on 160 of them)
 
-// A factor on logits, kept finite: 0 times it is 0 however large the queries' scale is.
-__device__ __forceinline__ float finite(float f) { return fminf(f, 3e38f); }
-// c tanh(x / c) log2(e) of x = y c / (2 log2(e)), through the exponential (the tanh instruction has 11 bits).
+// A factor on logits, kept positive and finite: 0 times it is 0 however large the queries' scale is, and the -inf of a masked row times it -inf however
+// small (logits that it raises stay below 1e-30: products of the operands are at most 2^23).
+__device__ __forceinline__ float finite(float f) { return fminf(fmaxf(f, 1.2e-38f), 3e38f); }
+// c tanh(x / c) log2(e) of x = y c / (2 log2(e)), through the exponential (the tanh instruction has 11 bits).  Off by c log2(e) 2^-21.3 at most: 6e-4
+// for the largest cap, as a factor on a weight no more than the weights' rounding (2^-12, 2^-9) lets pass.
 __device__ __forceinline__ float capped(float y, float c_log2e) { return c_log2e - __fdividef(2.f * c_log2e, 1.f + ex2(y)); }
 
 // What a unit is: a row tile of one sequence and KV head.

@@ -255,11 +255,9 @@ __device__ __forceinline__ void produce_rows(const Attend& a, Part& c, const Pla
       page = page1;
     }
   }
-  if (!ok) {                                                              // the CTA does not end with a copy on its way
-    for (int back = 1; back <= kRing; ++back) {
-      if (back <= k_sent) drain_wait(wait.bar(Smem::k_full + ((k_sent - back) & 1)), ((k_sent - back) >> 1) & 1, kWaitLimit);
-      if (back <= v_sent) drain_wait(wait.bar(Smem::v_full + ((v_sent - back) & 1)), ((v_sent - back) >> 1) & 1, kWaitLimit);
-    }
+  for (int back = 1; back <= kRing; ++back) {                             // the CTA does not end with a copy on its way, whoever gives up
+    if (back <= k_sent) drain_wait(wait.bar(Smem::k_full + ((k_sent - back) & 1)), ((k_sent - back) >> 1) & 1, kWaitLimit);
+    if (back <= v_sent) drain_wait(wait.bar(Smem::v_full + ((v_sent - back) & 1)), ((v_sent - back) >> 1) & 1, kWaitLimit);
   }
 }
 
@@ -336,10 +334,8 @@ __device__ __forceinline__ void issue(const Attend& a, Part& c, const Plan& plan
       ++parts_b;
     }
   }
-  if (!ok) {                                                              // see what was issued retire before tensor memory goes
-    commit(Smem::drain);
-    drain_wait(wait.bar(Smem::drain), 0, kWaitLimit);
-  }
+  commit(Smem::drain);                                                    // see what was issued retire before tensor memory goes, whoever gives up
+  drain_wait(wait.bar(Smem::drain), 0, kWaitLimit);
 }
 
 // ---- the softmax ------------------------------------------------------------------------------------------------------------

@@ -159,7 +159,9 @@ def attend_reference(cache, q, cu, scale, softcap=0.0):
         dz = 140 * 2.0 ** -24 * scale * (x.abs() @ k.abs().transpose(1, 2))
         if softcap:
             z = softcap * torch.tanh(z / softcap)
-            dz = dz + softcap * 2.0 ** -21                    # tanh through an exponential and a quotient
+            # bf16: tanh through an exponential and a quotient (base 2: a quarter of 2^y's 2^-22 twice, the quotient's 2^-22 twice, a sum's 2^-24);
+            # fp32: its own 2^-22, products and the argument's factor 3 times 2^-24
+            dz = dz + (z.abs() * 2.0 ** -21 if cache.dtype == torch.float32 else softcap * 2.0 ** -21)
         z = torch.where(sees, z, -math.inf)
         top = z.amax(-1, keepdim=True)
         w = torch.softmax(z, -1)
@@ -674,6 +676,62 @@ def test_two_contexts_on_two_streams(dq):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,fmt", TYPES)
+@pytest.mark.parametrize("cap", [1e-18, 0.3, 1000.0, 1024.0])
+def test_smallest_and_largest_caps(dq, dtype, fmt, cap):
+    ctx = context(dq, 8, 2, dtype)
+    cache = Cache(dq, dtype, fmt, 2, 16, [90, 7], [91, 57], wide=WIDE // 16)
+    for b, n in enumerate((91, 57)):
+        cache.fill(b, *(torch.randn(2, n, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(b)) for _ in "kv"))
+    q = torch.randn(51, 8, D, device="cuda", generator=torch.Generator(device="cuda").manual_seed(9)).to(dtype)
+    check_attend(dq, ctx, cache, q, [0, 1, 51], cap)
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,fmt", TYPES)
+def test_logits_whose_factor_underflows(dq, dtype, fmt):
+    """All of them 0 to fp32: every row seen weighs the same, those not seen nothing."""
+    ctx = dq.dapq_create(8, 2, 32, 4, 4096, dq.DAPQ_BF16 if dtype == torch.bfloat16 else dq.DAPQ_F32, 5.0e5, softmax_scale=1e-30)
+    cache = Cache(dq, dtype, fmt, 2, 16, [90, 7], [91, 57], wide=WIDE // 16, k_scale=2.0 ** -60)
+    v = [torch.randn(2, n, D, device="cuda") for n in (91, 57)]
+    for b in range(2):
+        cache.fill(b, torch.randn(*v[b].shape, device="cuda") * 2.0 ** -60, v[b])
+    q = (torch.randn(51, 8, D, device="cuda") * 2.0 ** -110).to(dtype)
+    out = torch.full_like(q, math.nan)
+    dq.dapq_paged_attend(ctx, cache.view, [0, 1, 51], q, out)
+    dq.dapq_poll_status(ctx)
+    for t, (b, n) in enumerate([(0, 91)] + [(1, 8 + i) for i in range(50)]):
+        x = cache.values(b, 0, n)[1]
+        want = x.mean(1).repeat_interleave(4, 0)
+        # weights 1 / n exactly (in 16 bits too: a power of two each), sums of n products
+        assert ((out[t].to(F64) - want).abs() <= half(dtype) * want.abs() + (n + 8) * 2.0 ** -24 * x.abs().mean(1).repeat_interleave(4, 0)).all(), t
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,fmt", TYPES)
+def test_queries_rotated_and_answered_in_place(dq, dtype, fmt):
+    ctx = context(dq, 8, 2, dtype)
+    cache = Cache(dq, dtype, fmt, 2, 16, [2000, 300, 5], [2001, 400, 5], wide=WIDE // 16)
+    for b, n in enumerate((2000, 300, 5)):
+        cache.fill(b, *(torch.randn(2, n, D, device="cuda") for _ in "kv"))
+    cu = [0, 1, 101, 101]
+    q = torch.randn(101, 8, D, device="cuda").to(dtype)
+    kv = torch.randn(2, 101, 2, D, device="cuda").to(dtype)
+    pos = torch.arange(101, dtype=torch.int32, device="cuda") + 7
+    turned, out = torch.empty_like(q), torch.empty_like(q)
+    dq.dapq_paged_append(ctx, cache.view, cu, kv[0], kv[1], pos, q, turned)
+    dq.dapq_paged_attend(ctx, cache.view, cu, turned, out)
+    dq.dapq_paged_append(ctx, cache.view, cu, kv[0], kv[1], pos, q, q)
+    assert torch.equal(q, turned)
+    dq.dapq_paged_attend(ctx, cache.view, cu, q, q)
+    assert torch.equal(q, out)
+    dq.dapq_poll_status(ctx)
+    dq.dapq_destroy(ctx)
+
+
+@gpu
 def test_refusals(dq):
     bf = torch.bfloat16
     ctx = context(dq, 8, 2, bf, max_batch=2)
@@ -706,7 +764,7 @@ def test_refusals(dq):
     refused(1, attend(cu=[1, 2, 2]))
     refused(1, attend(cu=[0, 2, 1]))
     refused(2, attend(cu=[0, 1, 1 << 30]))
-    for cap in (-1.0, math.nan, math.inf, 1e-19, 1e19):
+    for cap in (-1.0, math.nan, math.inf, 1e-19, 1025.0, 1e19):
         refused(1, attend(softcap=cap))
     refused(2, lambda: dq.dapq_paged_attend(ctx, cache.view, None, q, out.view(-1)[4:4 + 128].view(1, 1, D)))
     refused(1, lambda: dq.dapq_paged_append(ctx, cache.view, None, kv, kv, None, q, out))                       # queries without positions
@@ -720,6 +778,10 @@ def test_refusals(dq):
     back = torch.empty(2, 6, D, dtype=bf, device="cuda")
     refused(1, lambda: dq.dapq_paged_read(ctx, cache.view, None, [3, 4], [0, 3], back, back.clone()))           # one row too many
     refused(1, lambda: dq.dapq_paged_read(ctx, cache.view, None, [-1, 4], [0, 0], back, back.clone()))
+    for fn in (lambda: dq.dapq_paged_attend(ctx, cache.view, [0, 1], q, out), lambda: dq.dapq_paged_append(ctx, cache.view, [0, 1, 2, 2], kv, kv),
+               lambda: dq.dapq_paged_read(ctx, cache.view, None, [1], [0, 0], back, back.clone())):
+        with pytest.raises(AssertionError):                                                                     # offsets of another number of sequences
+            fn()
     n = dq.dapq_launch_count(ctx)
     dq.dapq_paged_attend(ctx, cache.view, [0, 0, 0], q, out)                                                    # nothing to do
     dq.dapq_paged_append(ctx, cache.view, [0, 0, 0], kv, kv)

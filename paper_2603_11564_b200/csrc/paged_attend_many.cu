@@ -31,9 +31,10 @@ struct Smem {
   static constexpr int q = 0, k = 2 * kTileBytes, v = k + kRing * kTileBytes, bars = v + kRing * kTileBytes;
   // barriers
   static constexpr int k_full = 0, k_empty = 2, v_full = 4, v_empty = 6, q_full = 8, s_full = 10, p_half = 12, p_full = 14, pv_done = 16, drain = 18, n_bars = 20;   // (one unused: the plan lies on 16 bytes)
-  static constexpr int plan = bars + 8 * n_bars, run = plan + (int)sizeof(Plan), parts = run + (int)sizeof(Run), tmem_ptr = parts + (kThreads / 32) * (int)sizeof(Part), abort_flag = tmem_ptr + 4, last_here = abort_flag + 4,
-                       total = last_here + 4;
+  static constexpr int plan = bars + 8 * n_bars, run = plan + (int)sizeof(Plan), parts = run + (int)sizeof(Run), other = parts + (kThreads / 32) * (int)sizeof(Part);
+  static constexpr int tmem_ptr = other + 128 * 8, abort_flag = tmem_ptr + 4, last_here = abort_flag + 4, total = last_here + 4;   // (other: see the epilogue)
 };
+static_assert(Smem::plan % 16 == 0 && Smem::run % 8 == 0 && Smem::parts % 8 == 0 && Smem::other % 8 == 0, "what lies there is read by 8 bytes");
 static_assert(Smem::total <= 232448, "exceeds the shared memory a CTA can opt in to");
 
 struct Many {                                         // geometry, for the shared scheduling
@@ -104,9 +105,13 @@ struct Wait {
 };
 
 // The 16-row pieces of a tile: lane p < 8 looks up the page of keys base + 16 p (a tile ahead of its use; -1 behind the limit).
-__device__ __forceinline__ int tile_page(const Attend& a, const Unit& u, int base, int lane) {
+__device__ __forceinline__ const int32_t* table_of(const Attend& a, const Unit& u) { return a.pg.table + (int64_t)u.b * a.pg.table_stride; }
+__device__ __forceinline__ int tile_page(const int32_t* table, int shift, int limit, int base, int lane) {
   const int row = base + 16 * lane;
-  return lane < 8 && row < u.limit ? __ldg(a.pg.table + (int64_t)u.b * a.pg.table_stride + (row >> a.pg.page_shift)) : -1;
+  return lane < 8 && row < limit ? __ldg(table + (row >> shift)) : -1;
+}
+__device__ __forceinline__ int tile_page(const Attend& a, const Unit& u, int base, int lane) {
+  return tile_page(table_of(a, u), a.pg.page_shift, u.limit, base, lane);
 }
 
 // ---- keys and values to shared memory -------------------------------------------------------------------------------------
@@ -273,13 +278,13 @@ template <bool kFp4>
 __device__ __forceinline__ void issue(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint32_t sbase, uint32_t tmem) {
   constexpr uint32_t idesc_s = kFp4 ? umma_idesc_f16(128, 128) : umma_idesc(128, 128), idesc_o = idesc_s | (1u << 16);   // (V: MN-major)
   const int lane = threadIdx.x & 31;
-  uint32_t done = 0, parts = 0, parts_b = 0, done_b = 0;
+  uint32_t done = 0, parts = 0, parts_b = 0, count[2] = {0, 0};           // tiles of keys so far, parts, parts with two tiles of rows, products of A and of B
   bool ok = true;
   auto commit = [&](int i) {
     if (elect_one()) tc_commit(wait.bar(i));
   };
-  auto scores = [&](uint32_t x, uint32_t st) {                            // S of tile x
-    const uint64_t q = umma_desc(sbase + Smem::q + x * kTileBytes), k = umma_desc(sbase + Smem::k + st * kTileBytes);
+  auto scores = [&](uint32_t x, uint32_t rows, uint32_t st) {             // S of tile x, which has the query rows of tile `rows`
+    const uint64_t q = umma_desc(sbase + Smem::q + rows * kTileBytes), k = umma_desc(sbase + Smem::k + st * kTileBytes);
     if (elect_one()) {
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks)
@@ -298,41 +303,49 @@ __device__ __forceinline__ void issue(const Attend& a, Part& c, const Plan& plan
     }
     __syncwarp();
   };
+  auto keys = [&](uint32_t t) { return wait.warp(Smem::k_full + (t & 1), (t >> 1) & 1); };
   for (bool on = true; on && ok; on = next_part(a, plan, run, c, lane)) {
     const int n = __shfl_sync(0xffffffffu, (int)(c.end - c.begin), 0);
     const bool two = __shfl_sync(0xffffffffu, c.u.rows - c.u.row0, 0) > 128;
-    ok = wait.warp(Smem::q_full, parts & 1) && (!two || wait.warp(Smem::q_full + 1, parts_b & 1)) && wait.warp(Smem::k_full + (done & 1), (done >> 1) & 1);
+    const int step = two ? 1 : 2;                                         // of the tiles of keys that a tile of rows takes
+    ok = wait.warp(Smem::q_full, parts & 1) && (!two || wait.warp(Smem::q_full + 1, parts_b & 1)) && keys(done);
     if (!ok) break;
     tc_fence_after();
-    scores(0, done & 1);
-    if (two) scores(1, done & 1);
+    scores(0, 0, done & 1);
+    if (two) scores(1, 1, done & 1);
     commit(Smem::k_empty + (done & 1));
+    if (!two && n > 1) {
+      ok = keys(done + 1);
+      if (!ok) break;
+      tc_fence_after();
+      scores(1, 0, (done + 1) & 1);
+      commit(Smem::k_empty + ((done + 1) & 1));
+    }
     for (int i = 0; i < n && ok; ++i) {
-      const uint32_t t = done + i, st = t & 1, st1 = st ^ 1;
+      const uint32_t t = done + i, st = t & 1, t1 = t + step;
+      const bool more = i + step < n;
       ok = wait.warp(Smem::v_full + st, (t >> 1) & 1);
-      if (ok && i + 1 < n) ok = wait.warp(Smem::k_full + st1, ((t + 1) >> 1) & 1);
+      if (ok && more) ok = keys(t1);
 #pragma unroll 1
-      for (uint32_t x = 0; x < (two ? 2u : 1u) && ok; ++x) {
-        const uint32_t parity = (x ? done_b + i : t) & 1;
+      for (uint32_t x = two ? 0 : i & 1; x < (two ? 2u : (i & 1) + 1u) && ok; ++x) {
+        const uint32_t parity = (x ? count[1] : count[0]) & 1;
         ok = wait.warp(Smem::p_half + x, parity);
         if (!ok) break;
         tc_fence_after();
-        outputs(x, st, 0, i > 0);
+        outputs(x, st, 0, i >= step);
         ok = wait.warp(Smem::p_full + x, parity);
         if (!ok) break;
         tc_fence_after();
         outputs(x, st, 4, true);
-        if (i + 1 < n) scores(x, st1);
+        if (more) scores(x, two ? x : 0, t1 & 1);
+        if (x) ++count[1]; else ++count[0];
       }
       commit(Smem::v_empty + st);
-      if (i + 1 < n) commit(Smem::k_empty + st1);
+      if (more) commit(Smem::k_empty + (t1 & 1));
     }
     done += n;
     ++parts;
-    if (two) {
-      done_b += n;
-      ++parts_b;
-    }
+    if (two) ++parts_b;
   }
   commit(Smem::drain);                                                    // see what was issued retire before tensor memory goes, whoever gives up
   drain_wait(wait.bar(Smem::drain), 0, kWaitLimit);
@@ -345,44 +358,57 @@ __device__ __forceinline__ void hide(uint32_t (&v)[32], int left, uint32_t gone)
   for (int j = 0; j < 32; ++j)
     if (j >= left || ((gone >> (j >> 4)) & 1u)) v[j] = 0xff800000u;
 }
-// The rows of a unit from the partial results of the CTAs that share it, in their order: a warp takes rows warp, warp + 8, .., and of these
-// kAtOnce together, whose loads are in flight together (one after the other they took a seventh of the kernel's time).
+// Row `row_of` of a unit from the parts of the CTAs that share it, in their order: pieces of 4 channels begin .. begin + count - 1 by this thread.  What a thread
+// waits for is latency, so 16 pieces are in flight.
 template <class E>
-__device__ __forceinline__ void merge_rows(const Attend& a, const Unit& u, const Share<E>& share, int warp, int lane) {
+__device__ __forceinline__ void join(const Attend& a, const Unit& u, const Share<E>& share, int row_of, int begin, int count) {
   constexpr int kAtOnce = 8;
-#pragma unroll 1
-  for (int y0 = warp; y0 < Many::kRows && u.row0 + y0 < u.rows; y0 += 8 * kAtOnce) {
-    float4 acc[kAtOnce];
-    float top[kAtOnce], sum[kAtOnce];
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      top[k] = kLowest;
-      sum[k] = 0.f;
-    }
-#pragma unroll 1
-    for (int x = 0; x < share.n; ++x) {
-      const float* from = x == 0 ? share.first : share.others + 2 * (int64_t)x * kSlotFloats<E>;
-      float4 v[kAtOnce];
-      float2 st[kAtOnce];
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const int y = min(y0 + 8 * k, Many::kRows - 1);
-        v[k] = __ldcg(reinterpret_cast<const float4*>(from + y * kHeadDim) + lane);
-        st[k] = __ldcg(reinterpret_cast<const float2*>(from + E::kSlotRows * kHeadDim) + y);
-      }
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const float now = fmaxf(top[k], st[k].x), f = ex2(top[k] - now), g = ex2(st[k].x - now);
-        top[k] = now;
-        sum[k] = fmaf(sum[k], f, g * st[k].y);
-        acc[k] = make_float4(fmaf(acc[k].x, f, g * v[k].x), fmaf(acc[k].y, f, g * v[k].y), fmaf(acc[k].z, f, g * v[k].z), fmaf(acc[k].w, f, g * v[k].w));
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k)
-      if (y0 + 8 * k < Many::kRows) write_row<E>(a, u, y0 + 8 * k, acc[k], top[k], sum[k], lane);
+  const int row = u.row0 + row_of;
+  auto from = [&](int x) { return x == 0 ? share.first : share.others + 2 * (int64_t)x * kSlotFloats<E>; };
+  auto stats = [&](int x) { return __ldcg(reinterpret_cast<const float2*>(from(x) + Many::kRows * kHeadDim) + row_of); };
+  if (row >= u.rows) return;
+  float top = kLowest, sum = 0.f;
+#pragma unroll 4
+  for (int x = 0; x < share.n; ++x) top = fmaxf(top, stats(x).x);
+#pragma unroll 4
+  for (int x = 0; x < share.n; ++x) {
+    const float2 st = stats(x);
+    sum = fmaf(ex2(st.x - top), st.y, sum);
   }
+  const int i = row / a.group, h = u.h * a.group + row - i * a.group;
+  const int64_t at = (int64_t)(a.start[u.b] + i) * a.n_q_heads + h;
+  const float down = sum == 0.f ? 0.f : (a.pg.fp4 ? a.pg.v_scale : 1.f) / sum;
+#pragma unroll 1
+  for (int c = begin; c < begin + count; c += kAtOnce) {
+    float4 acc[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int x0 = 0; x0 < share.n; x0 += 2) {
+      float4 v[2][kAtOnce];
+      float f[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int x = min(x0 + y, share.n - 1);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) v[y][k] = __ldcg(reinterpret_cast<const float4*>(from(x)) + (c + k) * Many::kRows + row_of);
+        f[y] = x0 + y < share.n ? ex2(stats(x).x - top) : 0.f;
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        if (f[y] == 0.f) continue;                                        // (0 times what may be an infinity that only other rows see)
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+          acc[k] = make_float4(fmaf(f[y], v[y][k].x, acc[k].x), fmaf(f[y], v[y][k].y, acc[k].y), fmaf(f[y], v[y][k].z, acc[k].z), fmaf(f[y], v[y][k].w, acc[k].w));
+      }
+    }
+    uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + at * kHeadDim + 4 * c);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; k += 2)
+      dst[k / 2] = make_uint4(pack(false, acc[k].x * down, acc[k].y * down), pack(false, acc[k].z * down, acc[k].w * down),
+                              pack(false, acc[k + 1].x * down, acc[k + 1].y * down), pack(false, acc[k + 1].z * down, acc[k + 1].w * down));
+  }
+  if (a.lse != nullptr && begin == 0) a.lse[at] = sum == 0.f ? -CUDART_INF_F : (top - E::kLift + log2f(sum)) * 0.69314718f;
 }
 template <bool kFp4, bool kCap>
 __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& plan, const Run& run, const Wait& wait, uint8_t* smem, uint32_t sbase,
@@ -395,44 +421,59 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
   bool ok = true;
   // (an aborting warp still walks every part: the others wait for it at the barriers, and the arrival counters have to come back to 0)
   for (bool on = true; on; on = next_part(a, plan, run, c, lane)) {
-    const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile, row = c.u.row0 + x * 128 + r;
-    const bool mine = x == 0 || c.u.rows - c.u.row0 > 128;                // (tile B of a unit of 128 rows or fewer has none)
+    // A unit of more than 128 rows: each tile has its own.  Of fewer: both have them, A over the even tiles of keys, B over the odd ones.
+    const bool two = c.u.rows - c.u.row0 > 128;
+    const int n = (int)(c.end - c.begin), first = (int)(c.begin - c.unit_begin) * Many::kTile, begin = two ? 0 : x, step = two ? 1 : 2;
+    const int row_of = two ? x * 128 + r : r, row = c.u.row0 + row_of;
     float m = kLowest, l = 0.f;
-    if (mine) {
-      // the row's query to shared memory
-      uint4 w[16] = {};
-      if (row < c.u.rows) {
-        const int i = row / a.group, h = c.u.h * a.group + row - i * a.group;
-        const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (int64_t)(a.start[c.u.b] + i) * a.q_stride + h * kHeadDim);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = __ldg(src + j);
-      }
+    if (begin < n) {
+      // The warp's 32 queries to shared memory, two rows at a time with 16 lanes each.
       float f = a.scale_log2e;
-      if (kFp4) {
-        uint32_t* raw = reinterpret_cast<uint32_t*>(w);
-        uint32_t top = 0;
+      uint4 w[16];
+      uint32_t mine_e = 0;
 #pragma unroll
-        for (int i = 0; i < 64; ++i) top = max(top, max((raw[i] << 16) & 0x7fffffffu, raw[i] & 0x7fff0000u));
-        const int e = top == 0 ? 127 : min(max((int)(top >> 23), 1), 253);
-        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-        for (int i = 0; i < 64; ++i) raw[i] = pack(true, __uint_as_float(raw[i] << 16) * down, __uint_as_float(raw[i] & 0xffff0000u) * down);
-        f *= __uint_as_float((uint32_t)e << 23) * a.pg.k_scale;
+      for (int j = 0; j < 16; ++j) {
+        const int y = row - lane + 2 * j + (lane >> 4);
+        w[j] = make_uint4(0, 0, 0, 0);
+        if (y < c.u.rows) {
+          const int i = y / a.group, h = c.u.h * a.group + y - i * a.group;
+          w[j] = __ldg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (int64_t)(a.start[c.u.b] + i) * a.q_stride + h * kHeadDim) + (lane & 15));
+        }
       }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (kFp4) {
+          uint32_t raw[4] = {w[j].x, w[j].y, w[j].z, w[j].w}, top = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max(top, max((raw[e] << 16) & 0x7fffffffu, raw[e] & 0x7fff0000u));
+#pragma unroll
+          for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const uint32_t e = top == 0 ? 127 : min(max(top >> 23, 1u), 253u), of_row = __shfl_sync(0xffffffffu, e, (lane & 1) << 4);
+          if (lane >> 1 == j) mine_e = of_row;
+          const float down = __uint_as_float((254u - e) << 23);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) raw[k] = pack(true, __uint_as_float(raw[k] << 16) * down, __uint_as_float(raw[k] & 0xffff0000u) * down);
+          w[j] = make_uint4(raw[0], raw[1], raw[2], raw[3]);
+        }
+        if (two || x == 0) sts128(piece(sbase + Smem::q + x * kTileBytes, (r - lane) + 2 * j + (lane >> 4), lane & 15), w[j]);
+      }
+      if (kFp4) f *= __uint_as_float(mine_e << 23) * a.pg.k_scale;
       if (kCap) f *= 2.f / a.softcap;
       f = finite(f);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) sts128(piece(sbase + Smem::q + x * kTileBytes, r, j), w[j]);
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(wait.bar(Smem::q_full + x));
+      if (two || x == 0) {
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(wait.bar(Smem::q_full + x));
+      }
 
-      const int lim = sees(a, c.u, x * 128 + r);
-      int page = tile_page(a, c.u, first, lane), ahead = 0;
-      for (int i = 0; i < n && ok; ++i, ++done, page = ahead) {
+      const int lim = sees(a, c.u, row_of);
+      const int32_t* table = table_of(a, c.u);                            // (the part lies in shared memory: what a step needs of it is kept here)
+      const int limit = c.u.limit, full = c.u.full;
+      int page = tile_page(table, a.pg.page_shift, limit, first + begin * Many::kTile, lane), ahead = 0;
+      for (int i = begin; i < n && ok; i += step, ++done, page = ahead) {
         const int base = first + i * Many::kTile;
         const uint32_t gone = __ballot_sync(0xffffffffu, lane < 8 && (unsigned)page >= (unsigned)a.pg.n_pages);   // (pieces behind the limit too)
-        if (i + 1 < n) ahead = tile_page(a, c.u, base + Many::kTile, lane);
+        if (i + step < n) ahead = tile_page(table, a.pg.page_shift, limit, base + step * Many::kTile, lane);
         ok = wait.warp(Smem::s_full + x, done & 1);
         if (!ok) break;
         tc_fence_after();
@@ -445,7 +486,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
 #pragma unroll
           for (int j = 0; j < 128; ++j) s[j] = __float_as_uint(capped(__uint_as_float(s[j]) * f, a.softcap * 1.44269504f));
         }
-        if (base + Many::kTile > c.u.full || gone) {
+        if (base + Many::kTile > full || gone) {
           const int left = lim - base;
 #pragma unroll
           for (int j = 0; j < 128; ++j)
@@ -467,7 +508,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
           const float now = fmaxf(m, top), alpha = ex2(m - now);
           m = now;
           l *= alpha;
-          if (i > 0) {                                                    // (the first product of a part starts O anew)
+          if (i > begin) {                                                // (the first product of a part starts O anew)
             ok = wait.warp(Smem::pv_done + x, (done - 1) & 1);
             if (!ok) break;
             tc_fence_after();
@@ -506,42 +547,82 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
         l += sum.x + sum.y;
       }
       if (ok) ok = wait.warp(Smem::pv_done + x, (done - 1) & 1);
-      if (ok) {
-        const Share<E> share(a, run, c);
-        tc_fence_after();
-        const bool out = row < c.u.rows;
-        const int i = row / a.group, h = c.u.h * a.group + row - i * a.group;
-        const int64_t at = (int64_t)(a.start[c.u.b] + i) * a.n_q_heads + h;
-        const float down = l == 0.f ? 0.f : (kFp4 ? a.pg.v_scale : 1.f) / l;
-        __nv_bfloat16* dst = (__nv_bfloat16*)a.out + at * kHeadDim;
-        float* part = share.mine + (x * 128 + r) * kHeadDim;
+      if (ok) tc_fence_after();
+    }
+    // Outputs, 64 channels at a time.  What B has of A's rows goes through shared memory (the tile of B's own queries), weighted by either's maximum.
+    const Share<E> share(a, run, c);
+    const bool both = !two && n > 1, writes = ok && begin < n && (two || x == 0), out = row < c.u.rows;
+    float2* const stats = reinterpret_cast<float2*>(smem + Smem::other) + r;
+    const uint32_t given = sbase + Smem::q + kTileBytes;
+    auto chunk = [&](int j) { return given + r * 256 + ((j ^ (r & 7)) << 4); };   // of 16 bytes, 0 .. 15
+    float fa = 1.f, fb = 0.f;
+    const int i = row / a.group, h = c.u.h * a.group + row - i * a.group;
+    const int64_t at = (int64_t)(a.start[c.u.b] + i) * a.n_q_heads + h;
+    __nv_bfloat16* dst = (__nv_bfloat16*)a.out + at * kHeadDim;
+    uint4* part = reinterpret_cast<uint4*>(share.mine) + row_of;           // (32 pieces of 4 channels of 256 rows: what a warp stores is contiguous)
 #pragma unroll 1
-        for (int p = 0; p < 4; ++p) {
-          uint32_t o[32];
-          tmem_ld32(to + 32 * p, o);
-          tmem_ld_wait_for(o);
-          // (a row that saw nothing has weights 0, and its sums may be 0 times an infinity that others see: its output is 0)
-          if (!out) continue;
-          if (share.alone) {
+    for (int p = 0; p < 4; ++p) {
+      if (both && (p & 1) == 0) {
+        if (x == 1) {
+          if (p == 0) *stats = make_float2(m, ok ? l : 0.f);
+#pragma unroll 1
+          for (int k = 0; k < 2 && ok; ++k) {
+            uint32_t o[32];
+            tmem_ld32(to + 32 * (p + k), o);
+            tmem_ld_wait_for(o);
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-              uint32_t y[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                y[e] = l == 0.f ? 0u : pack(false, __uint_as_float(o[j + 2 * e]) * down, __uint_as_float(o[j + 2 * e + 1]) * down);
-              *reinterpret_cast<uint4*>(dst + 32 * p + j) = make_uint4(y[0], y[1], y[2], y[3]);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) __stcg(reinterpret_cast<uint4*>(part + 32 * p + j), make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+            for (int j = 0; j < 8; ++j) sts128(chunk(8 * k + j), make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]));
           }
         }
-        if (out && share.alone && a.lse != nullptr) a.lse[at] = l == 0.f ? -CUDART_INF_F : (m - E::kLift + log2f(l)) * 0.69314718f;
-        if (!share.alone) __stcg(reinterpret_cast<float2*>(share.mine + Many::kSlotRows * kHeadDim) + x * 128 + r, make_float2(m, l));
-        tc_fence_before();
+        softmax_sync();
+        if (p == 0 && x == 0) {
+          const float2 b = *stats;
+          const float top = fmaxf(m, b.x);
+          fa = ex2(m - top);
+          fb = ex2(b.x - top);
+          l = l * fa + b.y * fb;
+          m = top;
+        }
       }
+      if (writes) {
+        const float down = l == 0.f ? 0.f : (kFp4 ? a.pg.v_scale : 1.f) / l;
+        uint32_t o[32];
+        tmem_ld32(to + 32 * p, o);
+        tmem_ld_wait_for(o);
+        if (both) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint4 w = lds128(chunk(8 * (p & 1) + j));
+            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float mine = fa == 0.f ? 0.f : __uint_as_float(o[4 * j + e]) * fa, its = fb == 0.f ? 0.f : __uint_as_float(v[e]) * fb;
+              o[4 * j + e] = __float_as_uint(mine + its);
+            }
+          }
+        }
+        // (a row that saw nothing has weights 0, and its sums may be 0 times an infinity that others see: its output is 0)
+        if (out && share.alone) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            uint32_t y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[e] = l == 0.f ? 0u : pack(false, __uint_as_float(o[j + 2 * e]) * down, __uint_as_float(o[j + 2 * e + 1]) * down);
+            *reinterpret_cast<uint4*>(dst + 32 * p + j) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        } else if (out) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) __stcg(part + (8 * p + j / 4) * Many::kRows, make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+        }
+      }
+      if (both && (p & 1) == 1) softmax_sync();
     }
-    const Share<E> share(a, run, c);
+    if (writes) {
+      if (out && share.alone && a.lse != nullptr) a.lse[at] = l == 0.f ? -CUDART_INF_F : (m - E::kLift + log2f(l)) * 0.69314718f;
+      if (!share.alone) __stcg(reinterpret_cast<float2*>(share.mine + Many::kSlotRows * kHeadDim) + row_of, make_float2(m, l));
+    }
+    tc_fence_before();
     if (!share.alone) {
       __threadfence();
       softmax_sync();
@@ -549,7 +630,7 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
       softmax_sync();
       if (*last_here) {
         __threadfence();
-        merge_rows<E>(a, c.u, share, warp, lane);
+        join<E>(a, c.u, share, row_of, two ? 0 : 16 * x, two ? 32 : 16);
         if (threadIdx.x == 0) a.sync[share.c0] = 0u;
       }
       softmax_sync();
@@ -600,16 +681,16 @@ paged_attend_many_kernel(const __grid_constant__ Attend a, const __grid_constant
   }
   __syncthreads();
   if (__shfl_sync(0xffffffffu, mine, 0)) {
-    // registers: 256 x 184 + 128 x 88 + 128 x 56, the 65536 that the block was launched with
+    // registers: 256 x 184 + 128 x 80 + 128 x 64, the 65536 that the block was launched with
     if (warp < 8) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
       softmax<kFp4, kCap>(a, c, plan, run, wait, smem, sbase, tmem);
     } else if (warp < 12) {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
       if (kFp4) produce_codes(a, c, plan, run, wait, sbase);
       else if (warp == 8) produce_rows(a, c, plan, run, wait, sbase, &tk, &tv);
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
       if (warp == 12) issue<kFp4>(a, c, plan, run, wait, sbase, tmem);
     }
   }

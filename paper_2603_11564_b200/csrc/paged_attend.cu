@@ -692,11 +692,12 @@ cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
 
 }  // namespace
 
-// Which sequences of a bf16 call go to the kernel for many query rows.  It takes rows by 128 and some 0.9e6 row-key pairs a microsecond, the one here
-// by 16 and 0.26e6, but 10 us less to begin and end.  So: those of 48 rows of a KV head and more (rounded up as either kernel does, these gain), if
-// the gain of all of them, by the rows that their tables have room for, is more than those 10 us.  Measured, 8 KV heads, 4 bits, here | there: 1 k keys
-// 24 .. 128 rows 15 .. 16 | 19 .. 27 us; 8 k keys 64 rows 28 | 32, 128 rows 46 | 46; 32 k keys 32 rows 45 | 49, 48 rows 59 | 51, 128 rows 126 | 69.
-constexpr double kFewRate = 0.26e6, kManyRate = 0.9e6, kManyCost = 10.0;
+// Which sequences of a bf16 call go to the kernel for many query rows.  It takes rows by 128 and 1.6e6 row-key pairs a microsecond, the one here by 16 and
+// 0.26e6, but it needs 13 us more to begin and end.  So: those of a KV head's rows (rounded up as either kernel does) that gain, if the gain of all of them, by
+// the rows that their tables have room for, is more than that.  Measured, 8 KV heads, here | there, 4 bits: 1 k keys 32 .. 256 rows 15 .. 16 | 22 .. 30 us; 3 k keys
+// 128 rows 24 | 27, 192 rows 32 | 31; 8 k keys 64 rows 28 | 30, 128 rows 46 | 32; 32 k keys 32 rows 45 | 43, 48 rows 59 | 43, 128 rows 126 | 47; bf16: 8 k keys
+// 64 rows 31 | 29, 128 rows 52 | 30; 32 k keys 32 rows 52 | 44, 128 rows 152 | 48.
+constexpr double kFewRate = 0.26e6, kManyRate = 1.6e6, kManyCost = 13.0;
 double gain_of_many(const Attend& a, int rows) {
   const double keys = (double)((int64_t)a.pg.table_stride << a.pg.page_shift) * a.n_kv_heads;
   return rows <= 16 ? 0.0 : keys * ((rows + 15) / 16 * 16 / kFewRate - (rows + 127) / 128 * 128 / kManyRate);
@@ -706,7 +707,8 @@ size_t attend_part_floats(int n_sm, bool bf16) {
   const size_t few = 2 * kSlotFloats<TensorEngine<true, 1>>, many = bf16 ? attend_many_part_floats() : 0;
   return min(n_sm, kMostSms) * (2 * few > many ? 2 * few : many);
 }
-size_t attend_sync_words(int n_sm) { return (size_t)2 * min(n_sm, kMostSms); }
+size_t attend_counters(int n_sm) { return (size_t)2 * min(n_sm, kMostSms); }
+size_t attend_sync_words(int n_sm) { return attend_counters(n_sm) + attend_many_words(min(n_sm, kMostSms)); }
 
 cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t, const Dims& dm, const void* q, int64_t q_stride, float softcap, void* out,
                                 float* lse, float* part, uint32_t* sync, int n_sm, int* status, long long wait_limit, cudaStream_t s, LaunchLog* log) {
@@ -733,9 +735,8 @@ cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t,
     log->end(s);
   }
   if (rows_many > 0 && e == cudaSuccess) {
-    log->begin(kKindPagedAttend, s);
-    e = launch_attend_many(many, n_sm, s);
-    log->end(s);
+    many.split = reinterpret_cast<Split*>(sync + attend_counters(n_sm));
+    e = launch_attend_many(many, n_sm, s, log);
   }
   return e != cudaSuccess ? e : cudaGetLastError();
 }

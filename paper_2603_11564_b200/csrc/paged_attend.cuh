@@ -12,6 +12,9 @@
 
 namespace dapq {
 
+// The unit that begins in a CTA's run and ends in another's (there is one at most): what the kernel that joins its parts has to know.
+struct Split { int32_t b, h, row0, rows, n, slot; };   // n: CTAs that share it, this one first (0: no such unit); slot: of the first's part
+
 struct Attend {
   PagedDev pg;
   int32_t batch;
@@ -25,12 +28,15 @@ struct Attend {
   long long wait_limit;
   int32_t n_q_heads, n_kv_heads, group;
   float scale_log2e, softcap;
-  int32_t tma;                                       // the pools can be described to TMA (paged_attend_many.cu)
+  // paged_attend_many.cu: whether the pools can be described to TMA, whether units are joined by a kernel of its own, and what that is told
+  int32_t tma, join;
+  Split* split;
 };
 
-// The kernel for many query rows (paged_attend_many.cu), and what its partial results take per CTA.
-cudaError_t launch_attend_many(const Attend& a, int n_sm, cudaStream_t s);
+// The kernel for many query rows (paged_attend_many.cu), what its partial results take per CTA, and the words of its Splits (behind the counters).
+cudaError_t launch_attend_many(const Attend& a, int n_sm, cudaStream_t s, LaunchLog* log);
 size_t attend_many_part_floats();
+size_t attend_many_words(int ctas);
 
 namespace {
 

@@ -623,7 +623,10 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
       if (!share.alone) __stcg(reinterpret_cast<float2*>(share.mine + Many::kSlotRows * kHeadDim) + row_of, make_float2(m, l));
     }
     tc_fence_before();
-    if (!share.alone) {
+    if (!share.alone && a.join) {
+      if (threadIdx.x == 0 && share.c0 == blockIdx.x)
+        a.split[blockIdx.x] = {c.u.b, c.u.h, c.u.row0, c.u.rows, share.n, 2 * (int)blockIdx.x + (c.unit_begin > run.begin ? 1 : 0)};
+    } else if (!share.alone) {
       __threadfence();
       softmax_sync();
       if (threadIdx.x == 0) *last_here = atomicAdd(a.sync + share.c0, 1u) == (uint32_t)(share.n - 1);
@@ -636,6 +639,66 @@ __device__ __forceinline__ void softmax(const Attend& a, Part& c, const Plan& pl
       softmax_sync();
     }
   }
+}
+
+// The same in a kernel of its own, for units that many CTAs share: they end together, and the last one would join all of their parts alone.  A block takes 32
+// rows of the unit that begins with one CTA.
+constexpr int kJoinThreads = 256, kJoinRows = 32, kJoinFrom = 3;         // kJoinFrom: CTAs a unit from which on it is used
+template <bool kFp4>
+__global__ void __launch_bounds__(kJoinThreads)
+paged_attend_join_kernel(const __grid_constant__ Attend a) {
+  using E = ManyOf<kFp4>;
+  __shared__ __align__(16) float acc_of[kJoinRows][kHeadDim + 4];
+  __shared__ float2 stat_of[kJoinRows];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r0 = blockIdx.y * kJoinRows;
+  pdl_wait();
+  pdl_trigger();
+  const Split s = a.split[blockIdx.x];
+  if (s.n == 0 || s.row0 + r0 >= s.rows) return;
+  // The first CTA's part lies where it says, the others' in the first of their two slots: they begin within the unit.
+  auto from = [&](int x) { return a.part + (x == 0 ? (int64_t)s.slot : 2 * ((int64_t)blockIdx.x + x)) * kSlotFloats<E>; };
+  auto stats = [&](int x) { return __ldcg(reinterpret_cast<const float2*>(from(x) + Many::kRows * kHeadDim) + r0 + lane); };
+  constexpr int kBatch = 4, kPieces = kHeadDim / 4 / (kJoinThreads / 32);
+  float top = kLowest, sum = 0.f;
+#pragma unroll 8
+  for (int x = 0; x < s.n; ++x) top = fmaxf(top, stats(x).x);
+  float4 acc[kPieces];
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) acc[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int x0 = 0; x0 < s.n; x0 += kBatch) {
+    float4 v[kBatch][kPieces];
+    float2 st[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int x = min(x0 + i, s.n - 1);
+      st[i] = stats(x);
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) v[i][p] = __ldcg(reinterpret_cast<const float4*>(from(x)) + (kPieces * warp + p) * Many::kRows + r0 + lane);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (x0 + i >= s.n) break;
+      const float f = ex2(st[i].x - top);
+      if (f == 0.f) continue;                                             // (0 times what may be an infinity that only other rows see)
+      sum = fmaf(f, st[i].y, sum);
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+        acc[p] = make_float4(fmaf(f, v[i][p].x, acc[p].x), fmaf(f, v[i][p].y, acc[p].y), fmaf(f, v[i][p].z, acc[p].z), fmaf(f, v[i][p].w, acc[p].w));
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) *reinterpret_cast<float4*>(&acc_of[lane][4 * (kPieces * warp + p)]) = acc[p];
+  if (warp == 0) stat_of[lane] = make_float2(top, sum);
+  __syncthreads();
+  Unit u = {};
+  u.b = s.b;
+  u.h = s.h;
+  u.row0 = s.row0;
+  u.rows = s.rows;
+#pragma unroll
+  for (int r = warp; r < kJoinRows; r += kJoinThreads / 32)
+    write_row<E>(a, u, r0 + r, *reinterpret_cast<const float4*>(&acc_of[r][4 * lane]), stat_of[r].x, stat_of[r].y, lane);
 }
 
 template <bool kFp4, bool kCap>
@@ -680,6 +743,7 @@ paged_attend_many_kernel(const __grid_constant__ Attend a, const __grid_constant
     if (warp == 0) run = r;
   }
   __syncthreads();
+  if (threadIdx.x == 0 && a.join) a.split[blockIdx.x] = {};
   if (__shfl_sync(0xffffffffu, mine, 0)) {
     // registers: 256 x 184 + 128 x 80 + 128 x 64, the 65536 that the block was launched with
     if (warp < 8) {
@@ -703,17 +767,33 @@ paged_attend_many_kernel(const __grid_constant__ Attend a, const __grid_constant
 }
 
 template <bool kFp4, bool kCap>
-cudaError_t go(const Attend& a, const CUtensorMap& tk, const CUtensorMap& tv, int n_sm, cudaStream_t s) {
+cudaError_t go(Attend& a, const CUtensorMap& tk, const CUtensorMap& tv, int n_sm, cudaStream_t s, LaunchLog* log) {
   cudaError_t e = cudaFuncSetAttribute(paged_attend_many_kernel<kFp4, kCap>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::total);
   if (e != cudaSuccess) return e;
-  return launch_pdl(paged_attend_many_kernel<kFp4, kCap>, dim3((unsigned)most_ctas<Many>(a, n_sm)), dim3(kThreads), Smem::total, s, 1, a, tk, tv);
+  const int ctas = (int)most_ctas<Many>(a, n_sm);
+  int64_t units = 0;
+  int rows = 0;
+  for (int b = 0; b < a.batch; ++b) {
+    units += (int64_t)a.n_kv_heads * ((a.n[b] * a.group + Many::kRows - 1) / Many::kRows);
+    rows = max(rows, min(a.n[b] * a.group, Many::kRows));
+  }
+  a.join = kJoinFrom * units <= ctas;
+  log->begin(kKindPagedAttend, s);
+  e = launch_pdl(paged_attend_many_kernel<kFp4, kCap>, dim3(ctas), dim3(kThreads), Smem::total, s, 1, a, tk, tv);
+  log->end(s);
+  if (e != cudaSuccess || !a.join) return e;
+  log->begin(kKindPagedAttend, s);
+  e = launch_pdl(paged_attend_join_kernel<kFp4>, dim3(ctas, (rows + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0, s, 1, a);
+  log->end(s);
+  return e;
 }
 
 }  // namespace
 
+size_t attend_many_words(int ctas) { return (size_t)ctas * sizeof(Split) / sizeof(uint32_t); }
 size_t attend_many_part_floats() { return 2 * (size_t)kSlotFloats<Many>; }
 
-cudaError_t launch_attend_many(const Attend& in, int n_sm, cudaStream_t s) {
+cudaError_t launch_attend_many(const Attend& in, int n_sm, cudaStream_t s, LaunchLog* log) {
   Attend a = in;
   if (a.wait_limit <= 0) a.wait_limit = ptx::kWaitLimit;
   CUtensorMap tk = {}, tv = {};
@@ -724,8 +804,8 @@ cudaError_t launch_attend_many(const Attend& in, int n_sm, cudaStream_t s) {
     const int box = (1 << pg.page_shift) < Many::kTile ? 1 << pg.page_shift : Many::kTile;
     a.tma = encode_tile_map(&tk, pg.k, false, 4, dims, strides, box) && encode_tile_map(&tv, pg.v, false, 4, dims, strides, box);
   }
-  if (a.softcap > 0.f) return a.pg.fp4 ? go<true, true>(a, tk, tv, n_sm, s) : go<false, true>(a, tk, tv, n_sm, s);
-  return a.pg.fp4 ? go<true, false>(a, tk, tv, n_sm, s) : go<false, false>(a, tk, tv, n_sm, s);
+  if (a.softcap > 0.f) return a.pg.fp4 ? go<true, true>(a, tk, tv, n_sm, s, log) : go<false, true>(a, tk, tv, n_sm, s, log);
+  return a.pg.fp4 ? go<true, false>(a, tk, tv, n_sm, s, log) : go<false, false>(a, tk, tv, n_sm, s, log);
 }
 
 }  // namespace dapq

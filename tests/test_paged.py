@@ -440,6 +440,8 @@ MANY = [
     (8, 1, 32, [127, 128, 129, 255], [16, 17, 15, 48], 0.0),
     (12, 4, 64, [3000], [100], 20.0),
     (8, 2, 16, [120, 20, 4000, 7], [33, 1, 3, 200], 0.0),     # sequences for either kernel in one call
+    (8, 8, 64, [500, 90, 0, 1300, 40, 700, 260, 3], [600] * 8, 0.0),
+    (16, 16, 32, [2000, 100, -1, 3000], [200, 100, 64, 130], 8.0),
 ]
 
 
@@ -560,25 +562,73 @@ def test_attend_reports_bad_pages_and_goes_on(dq, dtype, fmt):
     dq.dapq_destroy(ctx)
 
 
+UNITS = (8, 8, 64, [500, 90, 0, 1300, 40, 700, 260, 3], [600] * 8)     # more units than a third of the CTAs: joined where they are computed
+
+
 @gpu
 @pytest.mark.parametrize("fmt", ["native", "fp4"])
-def test_giving_up_in_the_kernel_for_many_rows(dq, fmt):
+@pytest.mark.parametrize("shape", [(8, 2, 16, [3000, 70], [100, 100]), (4, 2, 16, [2500], [30]), UNITS], ids=["parts", "both tiles", "units"])
+def test_giving_up_in_the_kernel_for_many_rows(dq, fmt, shape):
     """A limit of a cycle on its waits: a status, no hang, and the next call is right (its arrival counters are back at 0)."""
+    hq, hkv, rows, lens, new = shape
     bf = torch.bfloat16
-    ctx = context(dq, 8, 2, bf)
-    cache = Cache(dq, bf, fmt, 2, 16, [3000, 70], [3100, 170], wide=WIDE // 16)
-    for b, a in enumerate((3100, 170)):
-        cache.fill(b, *(torch.randn(2, a, D, device="cuda") for _ in "kv"))
-    q = torch.randn(200, 8, D, device="cuda").to(bf)
+    ctx = context(dq, hq, hkv, bf)
+    cache = Cache(dq, bf, fmt, hkv, rows, lens, [a + n for a, n in zip(lens, new)], wide=WIDE // rows)
+    cu = [0]
+    for b, (a, n) in enumerate(zip(lens, new)):
+        cache.fill(b, *(torch.randn(hkv, a + n, D, device="cuda") for _ in "kv"))
+        cu.append(cu[-1] + n)
+    q = torch.randn(cu[-1], hq, D, device="cuda").to(bf)
     out = torch.empty_like(q)
-    for _ in range(2):                    # (only a limit that is over before the first look at the clock is sure to run out)
+    times = 0
+    for _ in range(10):
         dq.dapq_set_wait_limit(ctx, 1)
-        dq.dapq_paged_attend(ctx, cache.view, [0, 100, 200], q, out)
-        with pytest.raises(dq.DapqError) as e:
+        dq.dapq_paged_attend(ctx, cache.view, cu, q, out)
+        try:
             dq.dapq_poll_status(ctx)
-        assert e.value.status == dq.DAPQ_ERR_TIMEOUT
+            gave_up = False
+        except dq.DapqError as e:
+            assert e.status == dq.DAPQ_ERR_TIMEOUT
+            gave_up = True
         dq.dapq_set_wait_limit(ctx, 0)
-        check_attend(dq, ctx, cache, q, [0, 100, 200])
+        right, _ = check_attend(dq, ctx, cache, q, cu)
+        # (a barrier is tried once before the clock is looked at, and the hardware may hold that try for as long as a short run's waits take: then
+        # nothing runs out, and the result has to be right)
+        assert gave_up or torch.equal(out, right)
+        times += gave_up
+        if times == 2:
+            break
+    assert times > 0 or len(cu) == 2
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["native", "fp4"])
+@pytest.mark.parametrize("shape", [(8, 2, 16, [3000, 70], [100, 1]), UNITS], ids=["parts", "units"])
+def test_many_query_rows_in_a_graph(dq, fmt, shape):
+    """Replayed twice, behind another capture that uses the same workspace."""
+    hq, hkv, rows, lens, new = shape
+    bf = torch.bfloat16
+    ctx = context(dq, hq, hkv, bf)
+    cache = Cache(dq, bf, fmt, hkv, rows, lens, [a + n for a, n in zip(lens, new)], wide=WIDE // rows)
+    cu = [0]
+    for b, (a, n) in enumerate(zip(lens, new)):
+        cache.fill(b, *(torch.randn(hkv, a + n, D, device="cuda") for _ in "kv"))
+        cu.append(cu[-1] + n)
+    q = [torch.randn(cu[-1], hq, D, device="cuda").to(bf) for _ in range(2)]
+    want = [check_attend(dq, ctx, cache, x, cu, 30.0)[0] for x in q]
+    outs, graphs, stream = [torch.empty_like(x) for x in q], [torch.cuda.CUDAGraph() for _ in q], torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        for x, out, graph in zip(q, outs, graphs):
+            with torch.cuda.graph(graph, stream=stream):
+                dq.dapq_paged_attend(ctx, cache.view, cu, x, out, softcap=30.0)
+        for _ in range(2):
+            for out, graph in zip(outs, graphs):
+                out.zero_()
+                graph.replay()
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    dq.dapq_poll_status(ctx, stream)
     dq.dapq_destroy(ctx)
 
 

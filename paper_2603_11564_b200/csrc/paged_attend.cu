@@ -693,15 +693,22 @@ cudaError_t go(const Attend& a, int n_sm, cudaStream_t s) {
 }  // namespace
 
 // Which sequences of a bf16 call go to the kernel for many query rows.  It takes rows by 128 and 1.6e6 row-key pairs a microsecond, the one here by 16 and
-// 0.26e6, but it needs 13 us more to begin and end.  So: those of a KV head's rows (rounded up as either kernel does) that gain, if the gain of all of them, by
-// the rows that their tables have room for, is more than that.  Measured, 8 KV heads, here | there, 4 bits: 1 k keys 32 .. 256 rows 15 .. 16 | 22 .. 30 us; 3 k keys
-// 128 rows 24 | 27, 192 rows 32 | 31; 8 k keys 64 rows 28 | 30, 128 rows 46 | 32; 32 k keys 32 rows 45 | 43, 48 rows 59 | 43, 128 rows 126 | 47; bf16: 8 k keys
-// 64 rows 31 | 29, 128 rows 52 | 30; 32 k keys 32 rows 52 | 44, 128 rows 152 | 48.
-constexpr double kFewRate = 0.26e6, kManyRate = 1.6e6, kManyCost = 13.0;
-double gain_of_many(const Attend& a, int rows) {
-  const double keys = (double)((int64_t)a.pg.table_stride << a.pg.page_shift) * a.n_kv_heads;
-  return rows <= 16 ? 0.0 : keys * ((rows + 15) / 16 * 16 / kFewRate - (rows + 127) / 128 * 128 / kManyRate);
-}
+// 0.26e6; a unit (a row tile, 256 rows there and 16 here) beyond a wave of CTAs costs 0.08 and 0.045 us; and it needs 10 us more to begin and end.  So:
+// those of a KV head's rows (rounded up as either kernel does) that gain, if the gain of all of them, by the rows that their tables have room for, is more
+// than that.  Measured, 8 KV heads, here | there, 4 bits: 1 k keys 32 .. 256 rows 15 .. 16 | 22 .. 30 us; 3 k keys 128 rows 24 | 27, 192 rows 32 | 31; 8 k keys 64 rows
+// 28 | 30, 128 rows 46 | 32; 32 k keys 32 rows 45 | 43, 48 rows 59 | 43, 128 rows 126 | 47; 8 sequences of 10 keys 64 rows 14 | 14, 96 rows 20 | 14, 60 of them
+// 44 | 47 (32 rows), 81 | 47 (64); bf16: 8 k keys 64 rows 31 | 29, 128 rows 52 | 30; 32 k keys 32 rows 52 | 44, 128 rows 152 | 48.
+struct Gain {
+  double pairs = 0.0, few_units = 0.0, many_units = 0.0;
+  Gain() = default;
+  Gain(const Attend& a, int rows) {
+    const double keys = (double)((int64_t)a.pg.table_stride << a.pg.page_shift) * a.n_kv_heads, few = (rows + 15) / 16, many = (rows + 127) / 128;
+    if (rows > 16) pairs = keys * (16 * few / 0.26e6 - 128 * many / 1.6e6);
+    few_units = a.n_kv_heads * few;
+    many_units = (double)a.n_kv_heads * ((rows + 255) / 256);
+  }
+  bool enough(int n_sm) const { return pairs + 0.045 * max(0.0, few_units - n_sm) - 0.08 * max(0.0, many_units - n_sm) > 10.0; }
+};
 
 size_t attend_part_floats(int n_sm, bool bf16) {
   const size_t few = 2 * kSlotFloats<TensorEngine<true, 1>>, many = bf16 ? attend_many_part_floats() : 0;
@@ -715,12 +722,19 @@ cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t,
   Attend few = {pg, t.batch, {}, {}, q, q_stride, out, lse, part, sync, status, wait_limit, dm.n_q_heads, dm.n_kv_heads, dm.group, dm.scale_log2e, softcap};
   Attend many = few;
   int rows_few = 0, rows_many = 0;
-  auto gain = [&](int b) { return dtype == DAPQ_BF16 ? gain_of_many(few, (t.cu[b + 1] - t.cu[b]) * dm.group) : 0.0; };
-  double all = 0.0;
-  for (int b = 0; b < t.batch; ++b) all += max(gain(b), 0.0);
+  auto gain = [&](int b) { return Gain(few, (t.cu[b + 1] - t.cu[b]) * dm.group); };
+  Gain all;
+  for (int b = 0; b < t.batch && dtype == DAPQ_BF16; ++b) {
+    const Gain g = gain(b);
+    if (g.pairs <= 0.0) continue;
+    all.pairs += g.pairs;
+    all.few_units += g.few_units;
+    all.many_units += g.many_units;
+  }
+  const bool to_many = all.enough(n_sm);
   for (int b = 0; b < t.batch; ++b) {
     const int n = t.cu[b + 1] - t.cu[b], rows = n * dm.group;
-    const bool is_many = all > kManyCost && gain(b) > 0.0;
+    const bool is_many = to_many && gain(b).pairs > 0.0;
     (is_many ? rows_many : rows_few) = max(is_many ? rows_many : rows_few, rows);
     few.start[b] = many.start[b] = t.cu[b];
     few.n[b] = is_many ? 0 : n;

@@ -257,9 +257,24 @@ __device__ __forceinline__ bool take_run(const Attend& a, const Plan& plan, Run&
   run.ctas = max((int64_t)1, min(most, run.total / E::kMinRun));
   // Short runs: whole units, or as many CTAs for every one of them, so that (units being of one length) none has pieces of two.  8 units of 1400
   // rows in bf16 15.0 -> 12.4 us, of 16 k 19.6 -> 16.0; a ragged batch of 8 x 8 units 103 -> 95.  (fp32 rows take longer: 16.5 -> 18.2 us with it.)
-  if (E::kEven && plan.units <= most && run.total < 16 * run.ctas) {
-    if (run.ctas < 2 * plan.units) run.ctas = min(run.total, plan.units);
-    else run.ctas -= (uint32_t)run.ctas % (uint32_t)plan.units;
+  // More units than CTAs: as many for each if some small number of them divides, and a CTA more where every unit is one tile, as none is cut then (256 such
+  // units 26 -> 14 us).
+  if (E::kEven && run.total < 16 * most) {
+    if (plan.units <= most) {
+      if (run.total < 16 * run.ctas) {
+        if (run.ctas < 2 * plan.units) run.ctas = min(run.total, plan.units);
+        else run.ctas -= (uint32_t)run.ctas % (uint32_t)plan.units;
+      }
+    } else if (plan.units == run.total) {
+      run.ctas = most;
+    } else {
+      const uint32_t units = (uint32_t)plan.units, each = (units + (uint32_t)most - 1) / (uint32_t)most;
+      for (uint32_t k = each; k < each + 4; ++k)
+        if (units % k == 0) {
+          run.ctas = units / k;
+          break;
+        }
+    }
   }
   if (blockIdx.x >= run.ctas) return false;
   run.begin = run.start(blockIdx.x);

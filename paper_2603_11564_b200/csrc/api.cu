@@ -42,7 +42,7 @@ struct dapq_ctx {
   int64_t sync_words = 0;
   int sync_turn = 0;
   float* attend_part = nullptr;  // partial outputs of paged_attend.cu
-  uint32_t* attend_sync = nullptr;   // its arrival counters, all 0 between calls
+  uint32_t* attend_sync = nullptr;   // its arrival counters, all 0 between calls, and what its join is told
   PruneBuffers prune = {};       // the pruned selection (sums == nullptr: not available)
   // staging for the host-buffer entry points (allocated on first use): two sets, so that the copies of one
   // layer run beside the kernels of the layer before

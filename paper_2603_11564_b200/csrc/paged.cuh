@@ -40,7 +40,7 @@ cudaError_t launch_paged_compact(int dtype, const PagedDev& pg, const CacheDev& 
 cudaError_t launch_paged_read(int dtype, const PagedDev& pg, const ReadRows& t, int n_kv_heads, void* k_out, void* v_out, int64_t out_head_stride,
                               int* status, cudaStream_t s, LaunchLog* log);
 
-// Attention (paged_attend.cu).  part: attend_part_floats(n_sm, bf16) floats; sync: attend_sync_words(n_sm) words, all 0 between calls.
+// Attention (paged_attend.cu).  part: attend_part_floats(n_sm, bf16) floats; sync: attend_sync_words(n_sm) words, 0 before the first call.
 size_t attend_part_floats(int n_sm, bool bf16);
 size_t attend_sync_words(int n_sm);
 cudaError_t launch_paged_attend(int dtype, const PagedDev& pg, const NewRows& t, const Dims& dm, const void* q, int64_t q_stride, float softcap, void* out,

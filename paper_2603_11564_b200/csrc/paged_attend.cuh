@@ -3,7 +3,8 @@
 // Work: (sequence, KV head, query row tile, key tile), numbered in this order.  Lengths are known on the device only, so every CTA of one
 // wave adds them up and takes an equal run of the numbers, whatever the lengths are.  A CTA's result for a unit (sequence, head,
 // row tile) is final if its run covers the unit; otherwise it goes to the workspace, and the last of the unit's CTAs to arrive
-// joins their results in CTA order, so that the result does not depend on who that is.  Nobody waits for another CTA.
+// joins their results in CTA order, so that the result does not depend on who that is (paged_attend_many.cu: or a kernel behind it).  Nobody waits for
+// another CTA.
 //
 // Softmax: base 2, against a maximum that is only moved when a logit exceeds it by more than kSlack.
 #pragma once

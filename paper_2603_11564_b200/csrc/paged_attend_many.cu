@@ -1,21 +1,24 @@
 // Attention over the paged cache for many query rows of a sequence and KV head (a chunk of new tokens): rows on the tall side of tcgen05
 // tiles, 4 n L H_q d flops against one reading of the cache per 256 rows.
 //
-// A CTA has two tiles of 128 query rows (A and B) over the same keys, 128 at a time.  Four warps bring keys and values to shared memory as
-// 16-bit tiles with the 128-byte swizzle (codes times scales where the cache has 4 bits: done once for 256 query rows); one warp
-// issues the MMAs; four warps a tile take the softmax, one row a thread.  S = Q K^T goes to tensor memory, is read whole by its row's thread,
-// and comes back as the weights P, 16-bit, in the same columns, from where the second MMA takes them as its left operand; O += P V stays
-// in tensor memory.  V's tile is the right operand with its keys down (MN-major), so nothing is transposed.  While a tile's rows are
-// exponentiated the tensor cores have the other tile's two products.
+// A CTA has two tiles of 128 query rows (A and B) over the same keys, 128 at a time; a unit of 128 rows and fewer is on both, A with the even tiles of keys and B with
+// the odd ones, joined through shared memory at the end.  Keys and values lie in shared memory as 16-bit tiles with the 128-byte swizzle: in 4 bits four warps turn
+// codes and scales into them, once for 256 query rows; in bf16 one warp has them copied by TMA.  One warp issues the MMAs; four warps a tile take the softmax,
+// one row a thread.  S = Q K^T goes to tensor memory, is read whole by its row's thread, and comes back as the weights P, 16-bit, in the same columns, from
+// where the second MMA takes them as its left operand; O += P V stays in tensor memory.  V's tile is the right operand with its keys down (MN-major), so nothing is
+// transposed.  While a tile's rows are exponentiated the tensor cores have the other tile's two products.
 //
 // Types as in paged_attend.cu: fp16 for 4-bit caches (keys, values exact; queries exact after a power of two a row; weights, 2^11 times what
 // they are, to 11 bits), bf16 for bf16 caches (weights to 8 bits).
 //
-// Measured: two sequences, 300 and 450 new tokens, 64 heads of 8 KV heads, 13 k and 15 k rows in 4 bits (333 GFLOP): 351 us, 950 TFLOP/s (the warp-level
-// kernel: 2082; a cuBLAS product of that size: 201 in a burst, 240 under the power cap).  A step (256 rows, 128 keys) takes some 3400 cycles: its 32 MMAs
-// 83 cycles each, and what a tile's chain leaves uncovered: logits from tensor memory 180, their maximum 600, the weights 2 x 750, two
-// products 1330, hand-overs 300.  Tried: the maximum only after the fact, weights again where it moved (460), exponentials by polynomial for a quarter
-// of the pairs (+0 .. +90: instructions, not the MUFU, are short), three more warps for the values (382).
+// Measured: two sequences, 300 and 450 new tokens, 64 heads of 8 KV heads, 13 k and 15 k rows in 4 bits (333 GFLOP): 350 us, 950 TFLOP/s (the warp-level
+// kernel: 2082; a cuBLAS product of that size: 201 in a burst, 240 under the power cap).  32 k rows, 8 KV heads: 128 query rows 47 us in 4 bits and 48 in bf16,
+// 256 rows 62 and 60 (the warp-level kernel 126, 152; 234, 285).  A step (256 rows, 128 keys) takes some 3640 cycles, of which the tensor cores and the MUFU
+// are busy 2048 each (128 x 128 x 16 in 64 cycles; 16 exponentials a cycle): a tile's chain is what it is, logits from tensor memory 190, their maximum 600, the
+// weights 1560, two products 780 and hand-overs, and two of them overlap.  Tried: S and P in columns of their own, so that a tile's next S is there in time
+// (370: the issuing warp, 60 cycles an MMA and 70 a barrier, is then what all wait for); two issuing warps, by product (391, with eight warps for the codes 374) or by
+// tile (436); S by 64 keys in two buffers (420: an MMA of 64 columns takes as long as one of 128); 16 warps of half a row a thread (421, registers); the
+// maximum only after the fact, weights again where it moved (460); exponentials by polynomial for an eighth to half of the pairs (363 .. 419).
 #include "paged_attend.cuh"
 
 namespace dapq {

@@ -229,7 +229,7 @@ __device__ __forceinline__ void make_plan(const Attend& a, Plan& plan, int lane)
       const int held = a.pg.len[b];
       plan.held[b] = held;
       tiles = tiles_of<E>(a, b, held, &units);
-      if (blockIdx.x == 0 && tiles > 0 && (int64_t)held + a.n[b] > (int64_t)a.pg.table_stride << a.pg.page_shift) atomicOr(a.status, kStatusBadPage);
+      if (blockIdx.x == 0 && tiles > 0 && held >= 0 && (int64_t)held + a.n[b] > (int64_t)a.pg.table_stride << a.pg.page_shift) atomicOr(a.status, kStatusBadPage);
     }
     if (tiles > 0) all_units += units;
     int64_t x = (int64_t)tiles * units;

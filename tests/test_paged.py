@@ -727,6 +727,28 @@ def test_two_contexts_on_two_streams(dq):
 
 @gpu
 @pytest.mark.parametrize("dtype,fmt", TYPES)
+@pytest.mark.parametrize("wide", [0, WIDE // 64])
+def test_more_new_rows_than_room_for_a_sequence_that_takes_no_part(dq, dtype, fmt, wide):
+    """Its table has two pages: nothing of it is skipped, as nothing of it is there; one that takes part is flagged."""
+    ctx = context(dq, 3, 3, dtype)
+    cache = Cache(dq, dtype, fmt, 3, 64, [0, -1], [6, 0], wide=wide)
+    cache.fill(0, *(torch.randn(3, 6, D, device="cuda") for _ in "kv"))
+    n = cache.table.shape[1] * 64 + 100 if wide == 0 else 300
+    q = torch.randn(6 + n, 3, D, device="cuda").to(dtype)
+    check_attend(dq, ctx, cache, q, [0, 6, 6 + n])
+    dq.dapq_paged_append(ctx, cache.view, [0, 0, n], *(torch.zeros(2, n, 3, D, dtype=dtype, device="cuda")))
+    dq.dapq_poll_status(ctx)
+    if wide == 0:
+        held = torch.tensor([0, 0], dtype=torch.int32, device="cuda")
+        cache.view.cache_len = held.data_ptr()
+        dq.dapq_paged_attend(ctx, cache.view, [0, 6, 6 + n], q, torch.empty_like(q))
+        with pytest.raises(dq.DapqError):
+            dq.dapq_poll_status(ctx)
+    dq.dapq_destroy(ctx)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,fmt", TYPES)
 @pytest.mark.parametrize("cap", [1e-18, 0.3, 1000.0, 1024.0])
 def test_smallest_and_largest_caps(dq, dtype, fmt, cap):
     ctx = context(dq, 8, 2, dtype)

@@ -55,16 +55,6 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t bdesc, 
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
@@ -355,12 +345,6 @@ __device__ __forceinline__ void issue(const Attend& a, Part& c, const Plan& plan
 }
 
 // ---- the softmax ------------------------------------------------------------------------------------------------------------
-// 32 logits, of which the first `left` count, less the 16 of the first or second half that are gone (two bits).
-__device__ __forceinline__ void hide(uint32_t (&v)[32], int left, uint32_t gone) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j >= left || ((gone >> (j >> 4)) & 1u)) v[j] = 0xff800000u;
-}
 // Row `row_of` of a unit from the parts of the CTAs that share it, in their order: pieces of 4 channels begin .. begin + count - 1 by this thread.  What a thread
 // waits for is latency, so 16 pieces are in flight.
 template <class E>
